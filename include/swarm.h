@@ -9,7 +9,8 @@
  *  -> turn the step's selection into per-SSD request queues               (Section 6.1)
  * and, around that path: the density pass over C that starts the clustering (Section 5.1, Steps 1-3),
  * cluster maintenance over the local window (Section 6.2), and retrieval through the medoid index
- * (Section 5.2 Tier 1, Section 6.1).
+ * (Section 5.2 Tier 1, Section 6.1).  What a model does with the entries stands beside it: attention over a paged cache (Section
+ * 2.3), the pages' copying, forking, compacting and freeing, and beam search's selection.
  *
  * Conventions that hold for every call below:
  *  - Every data pointer is a DEVICE pointer owned by the caller.  The library never frees,
@@ -83,6 +84,9 @@ typedef struct {
 #define SWARM_DEV_DUP_ENTRY   16u /* repeated entry within one selection         */
 #define SWARM_DEV_BAD_OFFSETS 32u /* bucket offsets not non-decreasing from 0 to at most cap */
 #define SWARM_DEV_OVERFLOW    64u /* a co-activation count passed INT32_MAX (it wrapped) */
+#define SWARM_DEV_BAD_PAGE   128u /* page id outside [0,P) where a row's tokens need one */
+#define SWARM_DEV_NO_PAGE    256u /* no free page or no table slot left for a row */
+#define SWARM_DEV_BAD_LEN    512u /* a row's length or a stream's token count out of range */
 
 /* Creates a context bound to HIP device `device` and to `hip_stream` (a hipStream_t; NULL is the
  * default stream).  The stream stays the caller's.  */
@@ -374,6 +378,134 @@ swarm_status swarm_step(swarm_ctx* ctx, const swarm_keys* keys, const void* q, i
                         float* out_scores, const int32_t* e2c, int32_t Nc, const int32_t* replicas, int32_t R, int32_t D,
                         const int32_t* weight, const uint32_t* resident, int32_t* q_off, int32_t* q_cluster,
                         int32_t* q_load, int32_t cap);
+
+/*
+ * A paged cache of keys and values: what the scored entries are the keys of.  A pool of P pages of `page` tokens each, every layer's
+ * part of a page split by KV head, so that one head's share of a page is one contiguous piece; and for each row (a stream, a beam) the
+ * ids of its pages in order.  Rows may share pages: refs counts how many hold a page, plus what the caller adds for pages that it pins.
+ * A page whose count is 0 is free.  The layout is the caller's memory; the calls below read and change it.
+ */
+typedef enum { SWARM_BF16 = 0, SWARM_FP16 = 1, SWARM_FP32 = 2 } swarm_dtype;
+typedef struct {
+    int32_t dtype;         /* SWARM_BF16 or SWARM_FP16                                                      */
+    void* k;               /* device, [L][P][H][page][d], 16-byte aligned                                   */
+    void* v;               /* the same                                                                      */
+    int32_t L, P, H;       /* layers, pages, KV heads                                                       */
+    int32_t page;          /* tokens per page: a power of two from 1 to 256                                 */
+    int32_t d;             /* head dimension: a multiple of 8, at most 256                                  */
+    const int32_t* table;  /* device, int32 [rows][cap]: page ids of each row in order, -1 behind the last  */
+    const int32_t* len;    /* device, int32 [rows]: tokens that each row holds                              */
+    const int32_t* refs;   /* device, int32 [P]: holders of each page (swarm_tree_attend does not read it)  */
+    int32_t rows, cap;     /* rows, and table slots of each                                                 */
+} swarm_cache;
+
+/*
+ * Attention of drafted tokens over a cache (Section 2.3: only the few highest-scoring entries take part in attention; the selected
+ * pages or tokens are those of swarm_score_select).  Row b of the cache is stream b's context, of which every drafted token sees
+ * all of X[b][h]; beside it drafted token i sees those drafted tokens of its stream that its mask names.  For query head h*G+g:
+ *     s_x = scale * sum_c q[b][i][h*G+g][c] * k_x[c]     over x in X[b][h] and the visible drafted tokens
+ *     out[b][i][h*G+g] = sum_x exp(s_x - m) v_x / sum_x exp(s_x - m),  m = max_x s_x,    lse = m + ln sum_x exp(s_x - m)
+ *   X[b][h] = the row's len tokens without a selection; the tokens of pages sel[b][h][0..n_sel) that lie below len
+ *   (SWARM_SEL_PAGES, positions in the row's table), or those tokens themselves (SWARM_SEL_TOKENS, positions in the row).
+ * A token that sees nothing, or scores of -inf only, gets out = 0 and lse = -inf.  lse joins attention over parts: entries that come
+ * in later (from an SSD) are attended over in a call of their own, and the two results weighted by exp(lse - joint lse).
+ * Products and sums are fp32; a weight enters its product with v as two terms of the cache's type (about 16 bits, so that the result
+ * is rounded once, at the end), the sum of weights in fp32.  What a token does not see never reaches its result, infinities
+ * and NaN included.
+ *
+ * layer        which of the cache's L layers.
+ * q            device, [B][T][H*G][d] in the cache's type, 16-byte aligned.   B <= rows streams, T drafted tokens each (1..256; one
+ *              decoded token is T = 1).   G >= 1 query heads per KV head, T * G <= 2^20.
+ * k_new, v_new device, [B][T][H][d], 16-byte aligned: keys and values of the drafted tokens, which are not in the cache yet
+ *              (swarm_cache_append puts the accepted ones there); both NULL: the tokens see the context alone.
+ * n_new        device, int32 [B], or NULL for T in every stream: out and lse of tokens i >= n_new[b] are left as they were, and no
+ *              token sees them.
+ * mask         device, uint32 [B][T][ceil(T/32)]: bit j % 32 of word j / 32 says whether token i sees token j (itself included).
+ *              NULL: a chain, token i sees the tokens 0..i.
+ * sel          device, int32 [B][H][n_sel] or NULL.  -1 is padding; entries should be distinct (one that is listed twice counts
+ *              twice); what lies behind the row's tokens counts for nothing.   unit: swarm_sel_unit.
+ * scale        a finite number.
+ * out          device, [B][T][H*G][d] in the cache's type, 16-byte aligned.   lse: device, fp32 [B][T][H*G], or NULL.
+ * A page id outside [0,P) drops its tokens (SWARM_DEV_BAD_PAGE); a selected position outside [-1, cap) or [-1, cap * page) is
+ * dropped (SWARM_DEV_BAD_ENTRY); a length outside [0, cap * page], or n_new outside [0, T], is cut to it (SWARM_DEV_BAD_LEN).
+ * The order of sums depends on the sizes alone: the same call gives the same bits.
+ * Errors: SWARM_EINVAL for NULL or misaligned required pointers, one of k_new and v_new without the other, sizes out of range, cap *
+ * page above 2^30, out or lse overlapping an input.
+ */
+typedef enum { SWARM_SEL_PAGES = 0, SWARM_SEL_TOKENS = 1 } swarm_sel_unit;
+swarm_status swarm_tree_attend(swarm_ctx* ctx, const swarm_cache* cache, int32_t layer, const void* q, const void* k_new,
+                               const void* v_new, int32_t B, int32_t T, int32_t G, const int32_t* n_new, const uint32_t* mask,
+                               const int32_t* sel, int32_t n_sel, int32_t unit, float scale, void* out, float* lse);
+
+/*
+ * Forking, freeing and reserving: row r of the new tables goes on as row parent[r] of the old ones (beams after a selection; -1 empties
+ * the row), with room[r] more tokens reserved.  With l = len[parent[r]], full = l / page, need = ceil((l + room[r]) / page), at most cap:
+ *   the first row (lowest r) of a parent keeps the parent's pages up to need, reserved ones among them; every other row of that
+ *   parent shares its full pages and takes new pages for the slots from full to need - 1; where l ends inside a page, the first
+ *   of them gets a copy of that page's l % page tokens, in all layers (so that need counts that page in any case).
+ *   refs_out = refs - what the old tables held + what the new ones hold.  New pages are the lowest ids whose refs_out would be 0
+ *   without them, in ascending order over (row, slot).
+ * Where pages run out, the slots that miss one stay -1 and SWARM_DEV_NO_PAGE is raised (a row whose partly filled page could not be
+ * copied ends at its last full page); the same flag where need exceeds cap.
+ * parent   device, int32 [rows]; a value outside [-1, rows) leaves the row as it is (as parent[r] = r) and raises SWARM_DEV_BAD_ENTRY.
+ * room     device, int32 [rows] (below 0 counts as 0), or NULL for 0.
+ * Outputs  table_out int32 [rows][cap], len_out int32 [rows], refs_out int32 [P]: written whole; none may overlap an input.  The
+ *          pool's new pages are written in place.  A page that two rows with different parents hold partly filled stays shared: such
+ *          tables do not come out of these calls.
+ * A length outside what the row's leading pages hold is cut to it (SWARM_DEV_BAD_LEN); page ids outside [0,P) end a row there
+ * (SWARM_DEV_BAD_PAGE).   Errors: SWARM_EINVAL for NULL or misaligned pointers, rows > 16384, rows * cap > 2^28, P > 2^26,
+ * overlapping outputs.
+ */
+swarm_status swarm_cache_fork(swarm_ctx* ctx, const swarm_cache* cache, const int32_t* parent, const int32_t* room,
+                              int32_t* table_out, int32_t* len_out, int32_t* refs_out);
+
+/*
+ * Appending: token i < n[b] of stream b goes behind what row b holds, to position len[b] + i, in every layer.  It is drafted token
+ * path[b][i]: the accepted path of a tree, moved together (any tokens in any order), or token i itself without a path.
+ *     len_out[b] = len[b] + n[b]    for b < B, len[b] for the other rows
+ * k_new, v_new device, [L][B][T][H][d] in the cache's type, 16-byte aligned, T >= 1: the drafted tokens of all layers.
+ * path         device, int32 [B][n_max], or NULL (n_max is T then).   n: device, int32 [B], 0..n_max, or NULL for n_max.
+ * len_out      device, int32 [rows]; must not overlap cache->len.
+ * A row takes tokens only up to where its reserved pages end (swarm_cache_fork reserves): the others are dropped, len_out counts what was taken, and
+ * SWARM_DEV_NO_PAGE is raised.  A path entry outside [0,T) is not written (SWARM_DEV_BAD_ENTRY: that position keeps what the page
+ * held); len outside [0, cap * page] or n outside [0, n_max] is cut to it (SWARM_DEV_BAD_LEN).
+ * Rows must not share the pages that they write to (after swarm_cache_fork they do not).  Errors: SWARM_EINVAL for NULL or
+ * misaligned required pointers, sizes out of range, B > rows, k_new or v_new overlapping the pool.
+ */
+swarm_status swarm_cache_append(swarm_ctx* ctx, const swarm_cache* cache, const void* k_new, const void* v_new, int32_t B, int32_t T,
+                                const int32_t* path, int32_t n_max, const int32_t* n, int32_t* len_out);
+
+/*
+ * Compacting: the n pages in use (refs > 0) come to stand at ids 0..n-1.  Those with an id of n or more move, in ascending order, to
+ * the free ids below n, in ascending order, in all layers; tables and counts follow.
+ * table_out int32 [rows][cap], refs_out int32 [P], live int32 [1] (n): written whole; none may overlap an input.  Table entries
+ * outside [0,P) stay as they are.  Errors: as swarm_cache_fork.
+ */
+swarm_status swarm_cache_compact(swarm_ctx* ctx, const swarm_cache* cache, int32_t* table_out, int32_t* refs_out, int32_t* live);
+
+/*
+ * Beam search's selection.  Each of B groups has K beams with running scores; a beam's candidates are the V tokens:
+ *     score(beam, token) = scores[b][beam] + x - ln sum_t exp(x_t),   x = logits[b][beam][token]
+ * in 64 bits from exponentials of 32 (the logarithm is good to about 1e-7), rounded to fp32 once, at the end.  A NaN logit counts as -inf, and
+ * so does a score that comes out as NaN.  A finished beam has one candidate, token eos with the beam's score as it is.
+ * The k best candidates of a group come out in descending score; equal scores are won by the lower beam, and within a
+ * beam by the higher logit, then by the lower token.  Where a group has fewer than k candidates, the rest is parent = token = -1 and score = -inf.
+ *
+ * logits     device, [B][K] rows of V values of `dtype` (any swarm_dtype), `stride` >= V elements apart.
+ * scores     device, fp32 [B][K].   finished: device, uint8 [B][K] (not 0: finished), or NULL; eos in [0,V) with it.
+ * out_score  device, fp32 [B][k];  out_parent  int32 [B][k]: b * K + beam, the row that the k-th best goes on from (as parent of
+ *            swarm_cache_fork where k = K);  out_token  int32 [B][k].
+ * hist, step, hist_out   the tokens so far, reordered: hist int32 [B*K][hist_cap], step int32 [1] (device), hist_out int32
+ *            [B*k][hist_cap]:  hist_out[r][0..step) = hist[parent[r]][0..step), hist_out[r][step] = token[r]; the rest, and rows without a
+ *            parent, are left as they were.  A step outside [0, hist_cap) is cut to [0, hist_cap], its token not written and SWARM_DEV_BAD_ENTRY raised.  All three
+ *            NULL: no histories.
+ * Errors: SWARM_EINVAL for NULL or misaligned pointers, B, K, V, k < 1, K > 64, k > 128, V > 2^24, B * K > 2^20, stride < V, eos outside [0,V)
+ * with finished, outputs that overlap an input.
+ */
+swarm_status swarm_beam_select(swarm_ctx* ctx, const void* logits, int32_t dtype, int64_t stride, const float* scores,
+                               const uint8_t* finished, int32_t eos, int32_t B, int32_t K, int32_t V, int32_t k, float* out_score,
+                               int32_t* out_parent, int32_t* out_token, const int32_t* hist, const int32_t* step, int32_t hist_cap,
+                               int32_t* hist_out);
 
 /*
  * Replay of a recorded call sequence.  The per-step work of the path is a handful of short kernels,

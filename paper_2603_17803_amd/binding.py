@@ -8,8 +8,9 @@ there is no CPU fallback.
 from __future__ import annotations
 
 import ctypes as C
+import dataclasses
 import os
-from typing import Optional, Tuple
+from typing import Any, Optional, Tuple
 
 from . import build as _build
 
@@ -18,19 +19,40 @@ SWARM_KEYS_TOKEN, SWARM_KEYS_PAGE_MINMAX = 0, 1
 SWARM_CHECK_IDX = 1
 SWARM_DEV_BAD_ENTRY, SWARM_DEV_BAD_CLUSTER, SWARM_DEV_BAD_SSD, SWARM_DEV_CAP, SWARM_DEV_DUP_ENTRY = 1, 2, 4, 8, 16
 SWARM_DEV_BAD_OFFSETS, SWARM_DEV_OVERFLOW = 32, 64
+SWARM_DEV_BAD_PAGE, SWARM_DEV_NO_PAGE, SWARM_DEV_BAD_LEN = 128, 256, 512
+SWARM_BF16, SWARM_FP16, SWARM_FP32 = 0, 1, 2
+SWARM_SEL_PAGES, SWARM_SEL_TOKENS = 0, 1
 (SWARM_WAY_NONE, SWARM_WAY_DENSE, SWARM_WAY_DENSE_STREAMED, SWARM_WAY_DENSE_STAGGERED, SWARM_WAY_DENSE_PIECES, SWARM_WAY_ROWS,
  SWARM_WAY_POPCOUNT, SWARM_WAY_DENSE_STAGGERED_STREAMED) = range(8)
 SWARM_WAY_QUEUE_LDS, SWARM_WAY_QUEUE_SORTED, SWARM_WAY_QUEUE_COMPARED = 16, 17, 18
 
 EXPORTS = ["swarm_create", "swarm_destroy", "swarm_last_error", "swarm_source_hash", "swarm_device_status", "swarm_last_way", "swarm_score", "swarm_score_select", "swarm_score_select_static",
            "swarm_coact_accumulate", "swarm_coact_build_density", "swarm_map_requests", "swarm_map_requests_streams", "swarm_coact_density", "swarm_window_assign", "swarm_score_select_indexed", "swarm_expand_clusters",
-           "swarm_submission_order", "swarm_step", "swarm_calibrate", "swarm_capture_begin", "swarm_capture_end",
+           "swarm_submission_order", "swarm_step", "swarm_tree_attend", "swarm_cache_fork", "swarm_cache_append", "swarm_cache_compact",
+           "swarm_beam_select", "swarm_calibrate", "swarm_capture_begin", "swarm_capture_end",
            "swarm_graph_launch", "swarm_graph_destroy"]
 
 
 class swarm_keys(C.Structure):
     _fields_ = [("kind", C.c_int32), ("data", C.c_void_p), ("H", C.c_int32), ("N", C.c_int32), ("d", C.c_int32),
                 ("G", C.c_int32)]
+
+
+class swarm_cache(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p), ("L", C.c_int32), ("P", C.c_int32), ("H", C.c_int32),
+                ("page", C.c_int32), ("d", C.c_int32), ("table", C.c_void_p), ("len", C.c_void_p), ("refs", C.c_void_p),
+                ("rows", C.c_int32), ("cap", C.c_int32)]
+
+
+@dataclasses.dataclass(frozen=True)
+class Cache:
+    """The tensors of a paged cache (swarm_cache): k, v [L][P][H][page][d] bf16 or fp16; table int32 [rows][cap], length int32 [rows],
+    refs int32 [P].  The calls that change it write the pool in place and return a Cache with new tables."""
+    k: Any
+    v: Any
+    table: Any
+    length: Any
+    refs: Any = None
 
 
 class SwarmError(RuntimeError):
@@ -72,6 +94,11 @@ def load() -> C.CDLL:
     L.swarm_score_select_indexed.argtypes = [vp, vp, vp, i32, vp, i32, i32, vp, vp]
     L.swarm_expand_clusters.argtypes = [vp, vp, i64, i32, i32, i32, vp, vp, i32, vp, vp, i32]
     L.swarm_submission_order.argtypes = [vp, vp, vp, i64, i32, i32, vp, vp, vp]
+    L.swarm_tree_attend.argtypes = [vp, C.POINTER(swarm_cache), i32, vp, vp, vp, i32, i32, i32, vp, vp, vp, i32, i32, C.c_float, vp, vp]
+    L.swarm_cache_fork.argtypes = [vp, C.POINTER(swarm_cache), vp, vp, vp, vp, vp]
+    L.swarm_cache_append.argtypes = [vp, C.POINTER(swarm_cache), vp, vp, i32, i32, vp, i32, vp, vp]
+    L.swarm_cache_compact.argtypes = [vp, C.POINTER(swarm_cache), vp, vp, vp]
+    L.swarm_beam_select.argtypes = [vp, vp, i32, i64, vp, vp, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, i32, vp]
     L.swarm_calibrate.argtypes = [vp, i32, vp, C.c_size_t, i32, C.POINTER(C.c_double)]
     L.swarm_capture_begin.argtypes = [vp]
     L.swarm_capture_end.argtypes = [vp, C.POINTER(vp)]
@@ -220,6 +247,32 @@ def swarm_map_requests_streams(ctx: int, idx: int, steps: int, B: int, H: int, k
     return load().swarm_map_requests_streams(C.c_void_p(ctx), C.c_void_p(idx), steps, B, H, k, N, C.c_void_p(e2c), Nc,
                                              C.c_void_p(replicas), R, D, C.c_void_p(weight), C.c_void_p(resident),
                                              C.c_void_p(q_off), C.c_void_p(q_cluster), C.c_void_p(q_load), cap)
+
+
+def swarm_tree_attend(ctx: int, cache: swarm_cache, layer: int, q: int, k_new: Optional[int], v_new: Optional[int], B: int, T: int, G: int,
+                      n_new: Optional[int], mask: Optional[int], sel: Optional[int], n_sel: int, unit: int, scale: float, out: int,
+                      lse: Optional[int]) -> int:
+    return load().swarm_tree_attend(ctx, C.byref(cache), layer, q, k_new, v_new, B, T, G, n_new, mask, sel, n_sel, unit, scale, out, lse)
+
+
+def swarm_cache_fork(ctx: int, cache: swarm_cache, parent: int, room: Optional[int], table_out: int, len_out: int, refs_out: int) -> int:
+    return load().swarm_cache_fork(ctx, C.byref(cache), parent, room, table_out, len_out, refs_out)
+
+
+def swarm_cache_append(ctx: int, cache: swarm_cache, k_new: int, v_new: int, B: int, T: int, path: Optional[int], n_max: int,
+                       n: Optional[int], len_out: int) -> int:
+    return load().swarm_cache_append(ctx, C.byref(cache), k_new, v_new, B, T, path, n_max, n, len_out)
+
+
+def swarm_cache_compact(ctx: int, cache: swarm_cache, table_out: int, refs_out: int, live: int) -> int:
+    return load().swarm_cache_compact(ctx, C.byref(cache), table_out, refs_out, live)
+
+
+def swarm_beam_select(ctx: int, logits: int, dtype: int, stride: int, scores: int, finished: Optional[int], eos: int, B: int, K: int, V: int,
+                      k: int, out_score: int, out_parent: int, out_token: int, hist: Optional[int], step: Optional[int], hist_cap: int,
+                      hist_out: Optional[int]) -> int:
+    return load().swarm_beam_select(ctx, logits, dtype, stride, scores, finished, eos, B, K, V, k, out_score, out_parent, out_token, hist, step,
+                                    hist_cap, hist_out)
 
 
 def swarm_capture_begin(ctx: int) -> int:
@@ -549,6 +602,131 @@ class Swarm:
                         self._dev(q_load, torch.int32, "q_load"), cap)
         self._check("swarm_step", rc)
         return out_idx, out_scores, out
+
+    def _cache(self, cache: Cache, refs: bool) -> swarm_cache:
+        """The C form of a cache after the checks of its tensors' shapes; `refs`: the call reads the counts."""
+        torch = self.torch
+        k = cache.k
+        if k.dim() != 5 or tuple(cache.v.shape) != tuple(k.shape) or cache.v.dtype is not k.dtype:
+            raise ValueError("k and v must be [L][P][H][page][d] of one type")
+        L, P, H, page, d = k.shape
+        if cache.table.dim() != 2 or cache.length.shape != (cache.table.shape[0],):
+            raise ValueError("table must be [rows][cap] and length [rows]")
+        if (refs or cache.refs is not None) and (cache.refs is None or cache.refs.shape != (P,)):
+            raise ValueError("refs must be [P]")
+        dtype = self._dtype(k, "k", (torch.bfloat16, torch.float16))
+        return swarm_cache(dtype, self._dev(k, None, "k"), self._dev(cache.v, None, "v"), L, P, H, page, d, self._dev(cache.table, torch.int32, "table"),
+                           self._dev(cache.length, torch.int32, "length"), None if cache.refs is None else self._dev(cache.refs, torch.int32, "refs"),
+                           cache.table.shape[0], cache.table.shape[1])
+
+    def _dtype(self, t, name: str, allowed) -> int:
+        torch = self.torch
+        if t.dtype not in allowed:
+            raise ValueError(f"{name} has dtype {t.dtype}, expected one of {allowed}")
+        return {torch.bfloat16: SWARM_BF16, torch.float16: SWARM_FP16, torch.float32: SWARM_FP32}[t.dtype]
+
+    def _opt(self, t, shape, dtype, name: str):
+        """Address of an optional tensor of a given shape; None stays None."""
+        if t is None:
+            return None
+        if t.shape != shape:
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+        return self._dev(t, dtype, name)
+
+    def tree_attend(self, cache: Cache, layer: int, q, k_new=None, v_new=None, n_new=None, mask=None, sel=None, unit: str = "page",
+                    scale: Optional[float] = None, out=None, lse=None, want_lse: bool = False):
+        """Attention of T drafted tokens (T = 1: one decoded token) of each stream over its row of the cache, or over the selected pages or
+        tokens of it, and over the drafted tokens that they see.  q [B][T][H*G][d] and k_new, v_new [B][T][H][d] in the cache's
+        type; n_new int32 [B]; mask int32 [B][T][ceil(T/32)] words (None: a chain); sel int32 [B][H][n] positions as score_select gives them, of
+        pages (unit 'page') or tokens ('token'); scale: d ** -0.5 unless given.  Returns (out [B][T][H*G][d], lse fp32 [B][T][H*G] or None)."""
+        torch = self.torch
+        c = self._cache(cache, False)
+        if q.dim() != 4 or q.shape[3] != c.d or q.shape[2] % c.H or not q.shape[2]:
+            raise ValueError(f"q has shape {tuple(q.shape)}, expected [B][T][H*G][d] with H = {c.H} and d = {c.d}")
+        B, T, HG, d = q.shape
+        if unit not in ("page", "token"):
+            raise ValueError(f"unit is {unit!r}, expected 'page' or 'token'")
+        if sel is not None and sel.dim() != 3:
+            raise ValueError("sel must be [B][H][n]")
+        if out is None:
+            out = torch.empty((B, T, HG, d), dtype=q.dtype, device=self.device)
+        if lse is None and want_lse:
+            lse = torch.empty((B, T, HG), dtype=torch.float32, device=self.device)
+        kind, words = cache.k.dtype, (torch.int32, torch.uint32)
+        n = 0 if sel is None else sel.shape[2]
+        rc = swarm_tree_attend(self.ctx, c, layer, self._dev(q, kind, "q"), self._opt(k_new, (B, T, c.H, d), kind, "k_new"),
+                               self._opt(v_new, (B, T, c.H, d), kind, "v_new"), B, T, HG // c.H, self._opt(n_new, (B,), torch.int32, "n_new"),
+                               self._opt(mask, (B, T, (T + 31) // 32), words, "mask"), self._opt(sel, (B, c.H, n), torch.int32, "sel"), n,
+                               SWARM_SEL_PAGES if unit == "page" else SWARM_SEL_TOKENS, d ** -0.5 if scale is None else scale,
+                               self._opt(out, q.shape, kind, "out"), self._opt(lse, (B, T, HG), torch.float32, "lse"))
+        self._check("swarm_tree_attend", rc)
+        return out, lse
+
+    def cache_fork(self, cache: Cache, parent, room=None, out=None) -> Cache:
+        """Row r goes on as row parent[r] (-1: emptied) with room[r] tokens reserved; parent, room int32 [rows].  Returns the cache with
+        its new tables; `out` = (table, length, refs) reuses the caller's tensors (not those of `cache`)."""
+        torch = self.torch
+        c = self._cache(cache, True)
+        table, length, refs = out if out is not None else (torch.empty_like(cache.table), torch.empty_like(cache.length), torch.empty_like(cache.refs))
+        rc = swarm_cache_fork(self.ctx, c, self._opt(parent, (c.rows,), torch.int32, "parent"), self._opt(room, (c.rows,), torch.int32, "room"),
+                              self._opt(table, (c.rows, c.cap), torch.int32, "table"), self._opt(length, (c.rows,), torch.int32, "length"),
+                              self._opt(refs, (c.P,), torch.int32, "refs"))
+        self._check("swarm_cache_fork", rc)
+        return dataclasses.replace(cache, table=table, length=length, refs=refs)
+
+    def cache_append(self, cache: Cache, k_new, v_new, n=None, path=None, out=None) -> Cache:
+        """Puts n[b] tokens of each stream (all without n) behind what row b holds, in every layer: token path[b][i], or i without a path.
+        k_new, v_new [L][B][T][H][d] in the cache's type; n int32 [B]; path int32 [B][n_max].  Returns the cache with its new lengths;
+        `out` = length reuses the caller's tensor (not that of `cache`)."""
+        torch = self.torch
+        c = self._cache(cache, False)
+        if k_new.dim() != 5 or path is not None and path.dim() != 2:
+            raise ValueError("k_new and v_new must be [L][B][T][H][d], path [B][n_max]")
+        B, T = k_new.shape[1], k_new.shape[2]
+        n_max = T if path is None else path.shape[1]
+        kind, shape = cache.k.dtype, (c.L, B, T, c.H, c.d)
+        length = torch.empty_like(cache.length) if out is None else out
+        rc = swarm_cache_append(self.ctx, c, self._opt(k_new, shape, kind, "k_new"), self._opt(v_new, shape, kind, "v_new"), B, T,
+                                self._opt(path, (B, n_max), torch.int32, "path"), n_max, self._opt(n, (B,), torch.int32, "n"),
+                                self._opt(length, (c.rows,), torch.int32, "length"))
+        self._check("swarm_cache_append", rc)
+        return dataclasses.replace(cache, length=length)
+
+    def cache_compact(self, cache: Cache, out=None) -> Tuple[Cache, Any]:
+        """Moves the pages in use to the low ids.  Returns (the cache with its new tables, live int32 [1]: how many are in use); `out` =
+        (table, refs, live) reuses the caller's tensors (not those of `cache`)."""
+        torch = self.torch
+        c = self._cache(cache, True)
+        table, refs, live = out if out is not None else (torch.empty_like(cache.table), torch.empty_like(cache.refs), torch.empty((1,), dtype=torch.int32, device=self.device))
+        rc = swarm_cache_compact(self.ctx, c, self._opt(table, (c.rows, c.cap), torch.int32, "table"), self._opt(refs, (c.P,), torch.int32, "refs"),
+                                 self._opt(live, (1,), torch.int32, "live"))
+        self._check("swarm_cache_compact", rc)
+        return dataclasses.replace(cache, table=table, refs=refs), live
+
+    def beam_select(self, logits, scores, k: int, finished=None, eos: int = -1, vocab: Optional[int] = None, hist=None, step=None, hist_out=None,
+                    out=None):
+        """The k best continuations of each group: logits [B][K][V] fp32, bf16 or fp16 (the first `vocab` of each row count), scores fp32
+        [B][K], finished uint8 [B][K]; hist int32 [B][K][cap], step int32 [1] and hist_out int32 [B][k][cap] reorder the tokens so far.
+        Returns (score fp32, parent int32, token int32), each [B][k]; `out` = such a triple reuses the caller's tensors."""
+        torch = self.torch
+        if logits.dim() != 3:
+            raise ValueError("logits must be [B][K][V]")
+        B, K, stride = logits.shape
+        V = stride if vocab is None else vocab
+        if out is None:
+            out = (torch.empty((B, k), dtype=torch.float32, device=self.device), torch.empty((B, k), dtype=torch.int32, device=self.device),
+                   torch.empty((B, k), dtype=torch.int32, device=self.device))
+        score, parent, token = out
+        if hist is not None and (hist.dim() != 3 or step is None or hist_out is None):
+            raise ValueError("hist must be [B][K][cap] and comes with step and hist_out")
+        cap = 0 if hist is None else hist.shape[2]
+        rc = swarm_beam_select(self.ctx, self._dev(logits, None, "logits"), self._dtype(logits, "logits", (torch.float32, torch.bfloat16, torch.float16)), stride,
+                               self._opt(scores, (B, K), torch.float32, "scores"), self._opt(finished, (B, K), torch.uint8, "finished"), eos, B, K, V, k,
+                               self._opt(score, (B, k), torch.float32, "score"), self._opt(parent, (B, k), torch.int32, "parent"),
+                               self._opt(token, (B, k), torch.int32, "token"), self._opt(hist, (B, K, cap), torch.int32, "hist"),
+                               self._opt(step, (1,), torch.int32, "step"), cap, self._opt(hist_out, (B, k, cap), torch.int32, "hist_out"))
+        self._check("swarm_beam_select", rc)
+        return out
 
     def calibrate(self, what: int, buf, reps: int = 5) -> float:
         """Measured rate of a minimal kernel (GB/s for the memory measurements over `buf`, TOP/s for the MFMA loop)."""

@@ -117,6 +117,9 @@ swarm_status swarm_destroy(swarm_ctx* ctx) {
     if (ctx->lists) (void)hipFree(ctx->lists);
     if (ctx->rank) (void)hipFree(ctx->rank);
     if (ctx->part) (void)hipFree(ctx->part);
+    if (ctx->pages) (void)hipFree(ctx->pages);
+    if (ctx->attend) (void)hipFree(ctx->attend);
+    if (ctx->beams) (void)hipFree(ctx->beams);
     for (auto& t : ctx->tile_orders) (void)hipFree(t.second);
     for (void* p : ctx->retired) (void)hipFree(p);
     if (ctx->dev_flags) (void)hipFree(ctx->dev_flags);
@@ -154,7 +157,8 @@ swarm_status swarm_last_way(const swarm_ctx* ctx, int32_t* count_way, int32_t* q
     if (count_way) *count_way = ctx->count_way;
     if (queue_way) *queue_way = ctx->queue_way;
     if (scratch_bytes)
-        *scratch_bytes = ctx->scores_bytes + ctx->cand_bytes + ctx->trace_bytes + ctx->lists_bytes + ctx->part_bytes + ctx->rank_bytes + ctx->totals_bytes;
+        *scratch_bytes = ctx->scores_bytes + ctx->cand_bytes + ctx->trace_bytes + ctx->lists_bytes + ctx->part_bytes + ctx->rank_bytes + ctx->totals_bytes +
+                         ctx->pages_bytes + ctx->attend_bytes + ctx->beams_bytes;
     return SWARM_OK;
 }
 

@@ -44,6 +44,12 @@ struct swarm_ctx {
     int count_way = SWARM_WAY_NONE, queue_way = SWARM_WAY_NONE;   // what the last count and queue were made by
     bool trace_lds_opt_in = false, syrk_lds_opt_in = false;   // large dynamic LDS enabled for this context's device
     uint32_t batched_lds_opt_in = 0;                          // the same, a bit per form of the many-stream scorer
+    void* pages = nullptr;         // page ids and counts of a fork or a compaction
+    size_t pages_bytes = 0;
+    void* attend = nullptr;        // partial results of an attention whose keys are divided
+    size_t attend_bytes = 0;
+    void* beams = nullptr;         // candidates of a beam selection
+    size_t beams_bytes = 0;
     uint32_t* dev_flags = nullptr; // sticky SWARM_DEV_* bits (one word)
     void* static_scratch = nullptr; // this device's copy of the library's static scratch array (address resolved at create)
     std::vector<std::pair<int, int32_t*>> tile_orders;   // co-activation tile schedules, one per tile count, never rewritten
@@ -91,6 +97,17 @@ swarm_status swarm_grow(swarm_ctx* ctx, void** buf, size_t* have, size_t bytes);
 // kept until the context goes, as its graph refers to it.
 swarm_status swarm_try_grow(swarm_ctx* ctx, void** buf, size_t* have, size_t bytes, bool* there);
 bool swarm_capturing(const swarm_ctx* ctx);
+
+// Scratch of the calls around the paged cache: as swarm_grow, and refused (not an error of the runtime) where the caller captures the
+// stream by its own means and it would have to grow.
+swarm_status swarm_scratch(swarm_ctx* ctx, void** buf, size_t* have, size_t bytes);
+swarm_status swarm_check_cache(swarm_ctx* ctx, const char* fn, const swarm_cache* cache);
+struct swarm_range {
+    const void* at;
+    size_t bytes;
+};
+bool swarm_overlap(const swarm_range* outs, int n_outs, const swarm_range* ins, int n_ins);   // an output meets an input, or another output
+static inline bool swarm_misaligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
 
 // Fixed scratch handed to the launchers in place of the context's growing buffers (for the entry point that
 // may not allocate): the winners of the sliced selection.

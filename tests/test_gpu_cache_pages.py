@@ -1,0 +1,382 @@
+"""Forking, appending and compacting of a paged cache against a plain implementation on the host, bit for bit."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+TYPES = {"bf16": torch.bfloat16, "fp16": torch.float16}
+
+
+@pytest.fixture(scope="module")
+def sw():
+    from paper_2603_17803_amd import binding
+    s = binding.Swarm(0)
+    yield s
+    assert s.device_status() == 0
+    s.close()
+
+
+class Host:
+    """A cache on the host: the pool as bit patterns [2][L][P][H][page][d]."""
+
+    def __init__(self, seed, L=2, P=64, H=2, page=16, d=16, rows=6, cap=8, dtype="bf16"):
+        self.rng = np.random.default_rng(seed)
+        self.L, self.P, self.H, self.page, self.d, self.rows, self.cap, self.t = L, P, H, page, d, rows, cap, TYPES[dtype]
+        self.pool = self.rng.integers(-2 ** 15, 2 ** 15, size=(2, L, P, H, page, d)).astype(np.int16)
+        self.table = np.full((rows, cap), -1, dtype=np.int32)
+        self.len = np.zeros(rows, dtype=np.int32)
+        self.refs = np.zeros(P, dtype=np.int32)
+
+    def fill(self, lens, shared=0, extra=0):
+        """Rows of the given lengths with pages in random order; the first `shared` pages are the same in all rows; `extra` reserved pages each."""
+        ids = list(self.rng.permutation(self.P))
+        prefix = [ids.pop() for _ in range(shared)]
+        for r, n in enumerate(lens):
+            held = -(-n // self.page)
+            assert held >= shared
+            row = prefix + [ids.pop() for _ in range(held - shared + extra)]
+            self.table[r, :len(row)] = row
+            self.len[r] = n
+            for p in row:
+                self.refs[p] += 1
+        return self
+
+    def device(self):
+        from paper_2603_17803_amd import binding
+        k, v = (torch.from_numpy(x.copy()).cuda().view(self.t) for x in self.pool)
+        return binding.Cache(k, v, *(torch.from_numpy(x.copy()).cuda() for x in (self.table, self.len, self.refs)))
+
+    def fork(self, parent, room=None):
+        """The definition, row by row."""
+        old, oldlen, page = self.table.copy(), self.len.copy(), self.page
+        parent = [r if not -1 <= p < self.rows else p for r, p in enumerate(parent)]
+        room = [0] * self.rows if room is None else [max(0, int(x)) for x in room]
+        good = lambda x: 0 <= x < self.P  # noqa: E731
+        held = [next((j for j in range(self.cap) if not good(row[j])), self.cap) for row in old]
+        length = [min(max(int(n), 0), h * page) for n, h in zip(oldlen, held)]
+        for row in old:
+            for x in row:
+                if good(x):
+                    self.refs[x] -= 1
+        self.table[:] = -1
+        first, copies, want = set(), [], []
+        for r, p in enumerate(parent):
+            self.len[r] = 0
+            if p < 0:
+                continue
+            n = length[p]
+            full, need = n // page, min(-(-(n + room[r]) // page), self.cap)
+            keep = full
+            if p not in first:
+                first.add(p)
+                keep = min(held[p], need)
+            elif n % page:
+                copies.append((r, full, old[p][full], n % page))
+            self.table[r, :keep] = old[p][:keep]
+            self.len[r] = n
+            for x in self.table[r, :keep]:
+                self.refs[x] += 1
+            want += [(r, j) for j in range(keep, need)]
+        free = [x for x in range(self.P) if self.refs[x] == 0]
+        for (r, j), x in zip(want, free):
+            self.table[r, j] = x
+            self.refs[x] = 1
+        for r, j, src, tail in copies:
+            dst = self.table[r, j]
+            if dst < 0:
+                self.len[r] = j * page
+            else:
+                self.pool[:, :, dst, :, :tail] = self.pool[:, :, src, :, :tail]
+        return self
+
+    def append(self, new, n, path):
+        B, T = new.shape[2], new.shape[3]
+        for b in range(B):
+            count = T if path is None else path.shape[1]
+            count = count if n is None else int(n[b])
+            for i in range(count):
+                pos = int(self.len[b])
+                src = i if path is None else int(path[b][i])
+                if pos // self.page >= self.cap or not 0 <= self.table[b, pos // self.page] < self.P:
+                    break
+                if 0 <= src < T:
+                    self.pool[:, :, self.table[b, pos // self.page], :, pos % self.page] = new[:, :, b, src]
+                self.len[b] += 1
+        return self
+
+    def compact(self):
+        live = [p for p in range(self.P) if self.refs[p] > 0]
+        n = len(live)
+        move = dict(zip([p for p in live if p >= n], [p for p in range(n) if self.refs[p] <= 0]))
+        for a, b in move.items():
+            self.pool[:, :, b] = self.pool[:, :, a]
+        self.table = np.array([[move.get(int(x), int(x)) for x in row] for row in self.table], dtype=np.int32)
+        refs = np.zeros_like(self.refs)
+        for p in live:
+            refs[move.get(p, p)] = self.refs[p]
+        self.refs = refs
+        return n
+
+    def same(self, cache):
+        torch.cuda.synchronize()
+        assert np.array_equal(cache.table.cpu().numpy(), self.table)
+        assert np.array_equal(cache.length.cpu().numpy(), self.len)
+        assert np.array_equal(cache.refs.cpu().numpy(), self.refs)
+        for got, want in zip((cache.k, cache.v), self.pool):
+            assert np.array_equal(got.view(torch.int16).cpu().numpy(), want)
+
+
+def i32(x):
+    return None if x is None else torch.tensor(np.asarray(x), dtype=torch.int32, device="cuda")
+
+
+def fork(sw, host, parent, room=None):
+    cache = host.device()
+    before = [x.clone() for x in (cache.table, cache.length, cache.refs)]
+    got = sw.cache_fork(cache, i32(parent), i32(room))
+    host.fork(parent, room).same(got)
+    for x, y in zip(before, (cache.table, cache.length, cache.refs)):
+        assert torch.equal(x, y), "an input was written"
+    return got
+
+
+@pytest.mark.parametrize("page", [1, 2, 16, 256])
+@pytest.mark.parametrize("parent", [[0, 1, 2, 3, 4, 5], [0, 0, 0, 0, 0, 0], [5, 5, 5, 2, 2, 0], [-1] * 6, [3, -1, 3, -1, 1, 1], [1, 2, 3, 4, 5, 0]])
+def test_fork_of_ragged_rows(sw, page, parent):
+    lens = [5 * page, 3 * page - page // 2, 0, 1, page, 2 * page + (page > 1)]
+    fork(sw, Host(page, page=page, P=90, d=8).fill(lens), parent)
+    fork(sw, Host(page + 1, page=page, P=90, d=8).fill(lens, extra=2), parent, [0, 1, page, 2 * page + 1, 0, -4])
+
+
+@pytest.mark.parametrize("d,H,L,dtype", [(8, 1, 1, "bf16"), (24, 3, 2, "fp16"), (80, 5, 1, "bf16"), (128, 8, 3, "bf16"), (256, 2, 1, "fp16")])
+def test_fork_of_beams_with_a_shared_context(sw, d, H, L, dtype):
+    h = Host(d, L=L, H=H, d=d, P=40, rows=8, cap=9, dtype=dtype).fill([70, 70, 77, 64, 79, 65, 80, 71], shared=4)
+    fork(sw, h, [4, 4, 4, 0, 2, 2, 4, 7], [1] * 8)
+    fork(sw, h, [0, 1, 1, 3, 3, 3, 6, 6], [40] * 8)
+
+
+def test_fork_reserves_from_nothing(sw):
+    h = Host(3, rows=4, cap=6, P=30)
+    fork(sw, h, [0, 1, 2, 3], [1, 0, 96, 33])
+    assert (h.table >= 0).sum(1).tolist() == [1, 0, 6, 3]
+    # a row that keeps its reserved pages, one that gives them back
+    fork(sw, h, [0, 1, 2, 3], [16, 1, 0, 40])
+
+
+def test_fork_keeps_pages_that_the_caller_pins(sw):
+    h = Host(4).fill([50, 20, 0, 0, 0, 0])
+    pinned = int(h.table[0, 1])
+    h.refs[pinned] += 1
+    fork(sw, h, [-1] * 6, None)
+    assert h.refs.sum() == 1 and h.refs[pinned] == 1
+    fork(sw, h, [0] * 6, [60 * 16] + [0] * 5)                       # more than the table has room for
+    assert sw.device_status() == 256
+
+
+@pytest.mark.parametrize("P", [9, 10, 11, 12, 15])
+def test_fork_when_pages_run_out(sw, P):
+    from paper_2603_17803_amd import binding as b
+    h = Host(P, P=P, rows=4, cap=8).fill([40, 40, 20, 0])
+    fork(sw, h, [0, 0, 0, 2], [8, 8, 8, 100])
+    # row 0 keeps 3 pages, rows 1 and 2 share two of them and take one each, row 3 keeps 2 and takes 6 for 120 tokens: 13 in all
+    assert sw.device_status() == (b.SWARM_DEV_NO_PAGE if P < 13 else 0)
+
+
+def test_fork_of_bad_data(sw):
+    from paper_2603_17803_amd import binding as b
+    h = Host(5).fill([40, 40, 20, 0, 7, 0])
+    fork(sw, h, [0, 6, -2, 3, 2 ** 31 - 1, -2 ** 31])
+    assert sw.device_status() == b.SWARM_DEV_BAD_ENTRY
+    for bad in (-7, 64, 2 ** 31 - 1):
+        h = Host(6).fill([40, 40, 20, 0, 7, 0])
+        h.refs[h.table[1, 1]] -= 1
+        h.table[1, 1] = bad
+        fork(sw, h, [1, 1, 0, 0, 4, 4], [20] * 6)
+        assert sw.device_status() == b.SWARM_DEV_BAD_PAGE | b.SWARM_DEV_BAD_LEN
+    for bad in (-1, 49, 2 ** 31 - 1):
+        h = Host(7).fill([40, 40, 20, 0, 7, 0])
+        h.len[1] = bad
+        fork(sw, h, [1, 1, 0, 0, 4, 4], [20] * 6)
+        assert sw.device_status() == b.SWARM_DEV_BAD_LEN
+
+
+@pytest.mark.parametrize("rows,P,cap", [(1, 1, 1), (1, 5000, 3), (300, 9000, 20), (1025, 4097, 3)])
+def test_fork_of_many_rows_and_pages(sw, rows, P, cap):
+    h = Host(rows, L=1, H=1, d=8, page=2, P=P, rows=rows, cap=cap)
+    h.fill([int(x) for x in h.rng.integers(0, 2 * min(cap, P // rows) + 1, size=rows)])
+    parent = h.rng.integers(-1, rows, size=rows)
+    fork(sw, h, parent, h.rng.integers(0, 3, size=rows) if rows > 1 and P > 4100 else None)
+    sw.device_status()
+
+
+@pytest.mark.parametrize("T,n_max,page,d,L,dtype", [(1, 0, 16, 128, 1, "bf16"), (5, 0, 16, 8, 2, "fp16"), (7, 3, 1, 16, 3, "bf16"), (64, 9, 16, 128, 2, "bf16"), (40, 33, 8, 80, 1, "fp16"), (3, 20, 4, 256, 2, "bf16")])
+def test_append_along_paths(sw, T, n_max, page, d, L, dtype):
+    B, rows, H = 5, 7, 3
+    cap = 40 // page + 40
+    h = Host(T + d, L=L, P=rows * cap, H=H, page=page, d=d, rows=rows, cap=cap, dtype=dtype)
+    h.fill([0, 1, page, 2 * page + page // 2, 3, 2, 0], extra=-(-40 // page))
+    rng = h.rng
+    new = rng.integers(-2 ** 15, 2 ** 15, size=(2, L, B, T, H, d)).astype(np.int16)
+    path = rng.integers(0, T, size=(B, n_max)) if n_max else None          # any order, tokens repeated
+    for n in (None, [0, 1, min(2, n_max or T), n_max or T, 1]):
+        cache = h.device()
+        got = sw.cache_append(cache, *(torch.from_numpy(x).cuda().view(h.t) for x in new), n=i32(n), path=i32(path))
+        assert np.array_equal(cache.length.cpu().numpy(), h.len)
+        h.append(new, n, path).same(got)
+        h.len[:] = cache.length.cpu().numpy()
+
+
+def test_append_of_more_than_a_row_can_take_and_of_bad_data(sw):
+    from paper_2603_17803_amd import binding as b
+    rng = np.random.default_rng(1)
+    new = rng.integers(-2 ** 15, 2 ** 15, size=(2, 2, 3, 40, 2, 16)).astype(np.int16)
+    dev = [torch.from_numpy(x).cuda().view(torch.bfloat16) for x in new]
+    h = Host(8).fill([20, 128, 0, 0, 0, 0])                                 # room for 12, none, none
+    got = sw.cache_append(h.device(), *dev)
+    h.append(new, None, None).same(got)
+    assert h.len.tolist() == [32, 128, 0, 0, 0, 0] and sw.device_status() == b.SWARM_DEV_NO_PAGE
+    h = Host(9).fill([20, 100, 3, 0, 0, 0], extra=1)
+    h.table[0, 2] = 64                                                      # not a page of the pool
+    got = sw.cache_append(h.device(), *dev, n=i32([30, 2, 1]))
+    h.append(new, [30, 2, 1], None).same(got)
+    assert h.len[0] == 32 and sw.device_status() == b.SWARM_DEV_NO_PAGE
+    h = Host(10).fill([20, 100, 3, 0, 0, 0], extra=1)
+    path = [[0, 40, 2], [-1, 5, 6], [2 ** 31 - 1, 1, 1]]
+    got = sw.cache_append(h.device(), *dev, path=i32(path))
+    h.append(new, None, np.array(path)).same(got)
+    assert sw.device_status() == b.SWARM_DEV_BAD_ENTRY
+    h = Host(11).fill([20, 100, 3, 0, 0, 0], extra=1)
+    good = h.len.copy()
+    h.len[0], h.len[2] = -4, 2 ** 30
+    cache = h.device()
+    got = sw.cache_append(cache, *dev, n=i32([2, -1, 3]))
+    h.len[0], h.len[2] = 0, 128
+    h.append(new, [2, 0, 3], None).same(got)
+    assert sw.device_status() == b.SWARM_DEV_BAD_LEN | b.SWARM_DEV_NO_PAGE
+    h.len[:] = good
+
+
+@pytest.mark.parametrize("P,live,rows,L,H,page,d", [(1, 0, 1, 1, 1, 1, 8), (1, 1, 1, 1, 1, 1, 8), (7, 3, 2, 2, 1, 4, 16), (64, 64, 3, 1, 2, 16, 8), (64, 0, 3, 1, 2, 16, 8), (300, 120, 4, 3, 2, 16, 80),
+                                                    (4096, 2000, 5, 1, 1, 1, 8), (4097, 4000, 5, 1, 1, 1, 8), (9001, 11, 2, 1, 1, 2, 8), (130, 65, 2, 2, 8, 16, 128)])
+def test_compact(sw, P, live, rows, L, H, page, d):
+    h = Host(P + live, L=L, P=P, H=H, page=page, d=d, rows=rows, cap=max(1, live))
+    used = h.rng.permutation(P)[:live]
+    h.refs[used] = h.rng.integers(1, 5, size=live)
+    for r in range(rows):
+        part = used[r * live // rows:(r + 1) * live // rows]
+        h.table[r, :len(part)] = part
+    cache = h.device()
+    before = [x.clone() for x in (cache.table, cache.refs)]
+    got, n = sw.cache_compact(cache)
+    # what lies above the live pages afterwards is free: not compared
+    assert h.compact() == live == int(n)
+    h.same(got)
+    for x, y in zip(before, (cache.table, cache.refs)):
+        assert torch.equal(x, y)
+    again, n = sw.cache_compact(got)
+    assert int(n) == live and torch.equal(again.table, got.table) and torch.equal(again.refs, got.refs)
+    h.same(again)
+
+
+def test_compact_leaves_odd_entries(sw):
+    h = Host(12).fill([40, 20, 0, 0, 0, 0])
+    h.table[0, 3:6] = [-9, 64, 2 ** 31 - 1]
+    h.refs[int(h.table[1, 0])] = -2                                        # counts as free
+    got, n = sw.cache_compact(h.device())
+    assert h.compact() == int(n)
+    h.same(got)
+
+
+def test_refusals(sw):
+    from paper_2603_17803_amd import binding as b
+    h = Host(13).fill([40, 20, 0, 0, 0, 0])
+    c = h.device()
+    new = torch.zeros((2, 3, 5, 2, 16), dtype=torch.bfloat16, device="cuda")
+    six = i32(range(6))
+    raw = sw._cache(c, True)
+
+    def cache(**kw):
+        out = b.swarm_cache(*[getattr(raw, f) for f, _ in b.swarm_cache._fields_])
+        for f, x in kw.items():
+            setattr(out, f, x)
+        return out
+
+    t, l, r = torch.empty_like(c.table), torch.empty_like(c.length), torch.empty_like(c.refs)
+    p = lambda x: x.data_ptr()  # noqa: E731
+    bad_caches = [dict(refs=None), dict(k=None), dict(table=None), dict(P=0), dict(page=3), dict(d=12), dict(dtype=2), dict(rows=0), dict(cap=0), dict(k=raw.k + 2)]
+    for kw in bad_caches + [dict(rows=16385)]:
+        assert b.swarm_cache_fork(sw.ctx, cache(**kw), p(six), None, p(t), p(l), p(r)) == b.SWARM_EINVAL, kw
+    for a in [(None, None, p(t), p(l), p(r)), (p(six), None, None, p(l), p(r)), (p(six), None, p(t), None, p(r)), (p(six), None, p(t), p(l), None),
+              (p(six), None, p(c.table), p(l), p(r)), (p(six), None, p(t), p(c.length), p(r)), (p(six), None, p(t), p(l), p(c.refs)), (p(six), None, p(t), p(t), p(r)),
+              (p(six), None, p(t), p(six), p(r)), (p(six), p(l), p(t), p(l), p(r)), (p(six) + 2, None, p(t), p(l), p(r)), (p(six), None, raw.k, p(l), p(r))]:
+        assert b.swarm_cache_fork(sw.ctx, raw, *a) == b.SWARM_EINVAL, a
+    live = i32([0])
+    for kw in bad_caches:
+        assert b.swarm_cache_compact(sw.ctx, cache(**kw), p(t), p(r), p(live)) == b.SWARM_EINVAL, kw
+    for a in [(None, p(r), p(live)), (p(t), None, p(live)), (p(t), p(r), None), (p(c.table), p(r), p(live)), (p(t), p(c.refs), p(live)), (p(t), p(r), p(r)), (p(t), p(r), p(live) + 1)]:
+        assert b.swarm_cache_compact(sw.ctx, raw, *a) == b.SWARM_EINVAL, a
+    for kw in bad_caches[1:]:
+        assert b.swarm_cache_append(sw.ctx, cache(**kw), p(new), p(new), 3, 5, None, 0, None, p(l)) == b.SWARM_EINVAL, kw
+    for a in [(None, p(new), 3, 5, None, 0, None, p(l)), (p(new), None, 3, 5, None, 0, None, p(l)), (p(new), p(new), 0, 5, None, 0, None, p(l)), (p(new), p(new), 7, 5, None, 0, None, p(l)),
+              (p(new), p(new), 3, 0, None, 0, None, p(l)), (p(new), p(new), 3, 5, p(six), 0, None, p(l)), (p(new), p(new), 3, 5, None, 0, None, None),
+              (p(new), p(new), 3, 5, None, 0, None, p(c.length)), (raw.k, p(new), 3, 5, None, 0, None, p(l)), (p(new) + 8, p(new), 3, 5, None, 0, None, p(l)),
+              (p(new), p(new), 3, 5, None, 0, p(l), p(l))]:
+        assert b.swarm_cache_append(sw.ctx, raw, *a) == b.SWARM_EINVAL, a
+    torch.cuda.synchronize()
+    h.same(c)
+    for f in [lambda: sw.cache_fork(c, six[:5].contiguous()), lambda: sw.cache_fork(c, six, out=(t, l, r[:3])), lambda: sw.cache_fork(b.Cache(c.k, c.v, c.table, c.length), six),
+              lambda: sw.cache_append(c, new[:1], new[:1]), lambda: sw.cache_append(c, new, new.half()), lambda: sw.cache_append(c, new, new, path=six),
+              lambda: sw.cache_compact(c, out=(t, r, i32([0, 0]))), lambda: sw.cache_fork(c, six.long())]:
+        with pytest.raises(ValueError):
+            f()
+
+
+def test_recorded_and_captured_steps_replay(sw):
+    """A step that forks, appends and compacts, recorded by the library and captured by torch; every replay against the host."""
+    from paper_2603_17803_amd import binding as b
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        s = b.Swarm(0, stream=stream)
+        start = Host(14, rows=6).fill([40, 33, 20, 7, 0, 16])
+        c = start.device()
+        parent, room = i32([0] * 6), i32([4] * 6)
+        new = torch.zeros((2, 6, 4, 2, 16), dtype=torch.bfloat16, device="cuda")
+        tables = [torch.empty_like(c.table) for _ in range(2)]
+        lens, refs, live = [torch.empty_like(c.length) for _ in range(2)], [torch.empty_like(c.refs) for _ in range(2)], i32([0])
+
+        def step():
+            x = s.cache_fork(c, parent, room, out=(tables[0], lens[0], refs[0]))
+            x = s.cache_append(x, new, new, out=lens[1])
+            return s.cache_compact(x, out=(tables[1], refs[1], live))[0]
+
+        step()
+        stream.synchronize()
+        s.capture_begin()
+        after = step()
+        recorded = s.capture_end()
+        captured = torch.cuda.CUDAGraph()
+        stream.synchronize()
+        with torch.cuda.graph(captured, stream=stream):
+            step()
+        rng = np.random.default_rng(2)
+        for replay in (lambda: s.graph_launch(recorded), captured.replay):
+            for turn in range(3):
+                h = Host(20 + turn, rows=6).fill([int(x) for x in rng.integers(0, 60, size=6)])
+                fresh, order, bits = h.device(), rng.integers(0, 6, size=6), rng.integers(-2 ** 15, 2 ** 15, size=(2, 6, 4, 2, 16)).astype(np.int16)
+                for x, y in ((c.k, fresh.k), (c.v, fresh.v), (c.table, fresh.table), (c.length, fresh.length), (c.refs, fresh.refs)):
+                    x.copy_(y)
+                parent.copy_(i32(order))
+                new.copy_(torch.from_numpy(bits).cuda().view(torch.bfloat16))
+                replay()
+                stream.synchronize()
+                h.fork(order, [4] * 6).append(np.stack([bits, bits]), None, None)
+                assert h.compact() == int(live)
+                h.same(after)
+                s.cache_compact(fresh)
+        assert s.device_status() == 0
+        b.swarm_graph_destroy(recorded)
+        del captured
+        stream.synchronize()
+        s.close()
