@@ -415,7 +415,7 @@ typedef struct {
  *
  * layer        which of the cache's L layers.
  * q            device, [B][T][H*G][d] in the cache's type, 16-byte aligned.   B <= rows streams, T drafted tokens each (1..256; one
- *              decoded token is T = 1).   G >= 1 query heads per KV head, T * G <= 2^20.
+ *              decoded token is T = 1).   G query heads per KV head (1..1024).
  * k_new, v_new device, [B][T][H][d], 16-byte aligned: keys and values of the drafted tokens, which are not in the cache yet
  *              (swarm_cache_append puts the accepted ones there); both NULL: the tokens see the context alone.
  * n_new        device, int32 [B], or NULL for T in every stream: out and lse of tokens i >= n_new[b] are left as they were, and no
@@ -430,7 +430,8 @@ typedef struct {
  * dropped (SWARM_DEV_BAD_ENTRY); a length outside [0, cap * page], or n_new outside [0, T], is cut to it (SWARM_DEV_BAD_LEN).
  * The order of sums depends on the sizes alone: the same call gives the same bits.
  * Errors: SWARM_EINVAL for NULL or misaligned required pointers, one of k_new and v_new without the other, sizes out of range, cap *
- * page above 2^30, out or lse overlapping an input.
+ * page above 2^30, P * H * page or B * T * H above 2^32 - 2, B * H contexts of up to 2^31 times 128 keys or more (by the table's width, or
+ * n_sel), out or lse overlapping an input.
  */
 typedef enum { SWARM_SEL_PAGES = 0, SWARM_SEL_TOKENS = 1 } swarm_sel_unit;
 swarm_status swarm_tree_attend(swarm_ctx* ctx, const swarm_cache* cache, int32_t layer, const void* q, const void* k_new,
