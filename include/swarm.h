@@ -430,7 +430,7 @@ typedef struct {
  * dropped (SWARM_DEV_BAD_ENTRY); a length outside [0, cap * page], or n_new outside [0, T], is cut to it (SWARM_DEV_BAD_LEN).
  * The order of sums depends on the sizes alone: the same call gives the same bits.
  * Errors: SWARM_EINVAL for NULL or misaligned required pointers, one of k_new and v_new without the other, sizes out of range, cap *
- * page above 2^30, P * H * page or B * T * H above 2^32 - 2, B * H contexts of up to 2^31 times 128 keys or more (by the table's width, or
+ * page above 2^30, a layer of k, or k_new, of 64 GiB or more, B * H contexts of up to 2^31 times 128 keys or more (by the table's width, or
  * n_sel), out or lse overlapping an input.
  */
 typedef enum { SWARM_SEL_PAGES = 0, SWARM_SEL_TOKENS = 1 } swarm_sel_unit;

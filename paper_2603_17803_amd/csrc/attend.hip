@@ -26,7 +26,6 @@ typedef __attribute__((address_space(3))) v4s lds_v4s;
 
 constexpr int UNIT = 128;                        // keys of a unit, 32 for each wave
 constexpr int LISTED = 2048;                     // keys whose rows are looked up at a time
-constexpr uint32_t NO_ROW = 0xffffffffu;
 
 struct attend_args {
     const uint16_t *k, *v, *q, *k_new, *v_new;   // k, v: the layer's part of the pool
@@ -99,7 +98,7 @@ __device__ __forceinline__ stream stream_of(const attend_args& a, int b, bool te
 }
 __device__ __forceinline__ int token_of(const attend_args& a, int row) { return a.G == 1 ? row : (int)__umulhi((uint32_t)row, a.per_g); }
 
-// Sum over the lower threads of a workgroup of four waves, and over all of them.
+// Sum over the lower threads of a workgroup, and over all of them.
 __device__ __forceinline__ int block_before(int v, int* waves, int* total) {
     int x = v;
     const int lane = threadIdx.x % 64, w = threadIdx.x / 64;
@@ -110,25 +109,27 @@ __device__ __forceinline__ int block_before(int v, int* waves, int* total) {
     __syncthreads();
     if (lane == 63) waves[w] = x;
     __syncthreads();
-    int below = 0;
-    for (int i = 0; i < w; ++i) below += waves[i];
-    *total = waves[0] + waves[1] + waves[2] + waves[3];
+    int below = 0, sum = 0;
+    for (int i = 0; i < (int)blockDim.x / 64; ++i) {
+        below += i < w ? waves[i] : 0;
+        sum += waves[i];
+    }
+    *total = sum;
     return below + x - v;
 }
 // Units of a part: part p takes units p * quota to (p + 1) * quota of the line, and unit g stands in part g / quota.
 __device__ __forceinline__ int quota_of(const attend_args& a, int units) { return max(1, (units + a.parts - 1) / a.parts); }
 
 // What a wave carries of NR * 16 query rows: lane l has row l % 16 of each 16, and of the sums of values the channels
-// 16 c + 4 (l / 16) + 0..3.
+// 16 c + 4 (l / 16) + 0..3.  KT keys are taken at a time.
 //   TERMS: how many terms of the cache's type a weight enters its product with v as.  Two are a weight to 2^-16 and more,
 //   and cost half as many products again.
-template <bool BF16, int DP, int NR, int TERMS, bool FULL>
+template <bool BF16, int DP, int NR, int KT, int TERMS, bool FULL>
 struct flash {
-    static constexpr int KS = DP / 32, CT = DP / 16, VI = DP / 16;
-    static constexpr int VLD = DP + 16;                 // LDS row of V in elements: 32 bytes behind each, so that 16 rows' reads meet no bank twice
-    static constexpr int LPR = DP / 8, RPI = 64 / LPR;  // lanes on a row of V, rows that a wave moves at a time
-    v4i qf[NR][KS], kf[2][KS], vr[VI], pf[NR][TERMS];
-    v4f o[NR][CT], sc[NR][2];
+    static constexpr int KS = DP / 32, CT = DP / 16;
+    static constexpr int VLD = DP + 16;          // LDS row of V in elements: 32 bytes behind each, so that 16 rows' reads meet no bank twice
+    v4i qf[NR][KS], pf[NR][TERMS][KT / 32];
+    v4f o[NR][CT], sc[NR][KT / 16];
     float m[NR], l[NR];
 
     __device__ __forceinline__ void start(const attend_args& a, int b, int h, int row0, int drafted) {
@@ -148,26 +149,111 @@ struct flash {
             for (int c = 0; c < CT; ++c) o[n][c] = v4f{0.f, 0.f, 0.f, 0.f};
         }
     }
-    // Pieces behind the head dimension read another one, and count as 0.
-    __device__ __forceinline__ void load_k(const uint16_t* base, const uint32_t* rows, int d) {
+    // V^T of 16 channels and 32 keys, as the operand of the second product: elements 0..3 and 4..7 of lane l are keys 4 (l / 16) + 0..3 and
+    // 16 more.
+    static __device__ __forceinline__ v4i get_v(const uint16_t* vs, int c) {
         const int col = threadIdx.x % 16, quad = threadIdx.x % 64 / 16;
+        const uint16_t* from = vs + (quad * 4 + col / 4) * VLD + col % 4 * 4 + c * 16;
+        const v2i x = __builtin_bit_cast(v2i, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(from)));
+        const v2i y = __builtin_bit_cast(v2i, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(from + 16 * VLD)));
+        return v4i{x[0], x[1], y[0], y[1]};
+    }
+    // The weights of KT keys; sees[j]: which of the keys 32 j to 32 j + 31 the lane's rows see.  The maximum that weights refer to is raised only
+    // when one of the 16 rows has outgrown it by 2^8: a row's weights stay below that, which no sum here minds, and most
+    // tiles rescale nothing.
+    __device__ __forceinline__ void weigh(float scale_log2, const uint32_t* sees, bool all) {
+        const int quad = threadIdx.x % 64 / 16;
+        float mx[NR];
+        bool grown = false;
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            uint32_t row = rows[k * 16 + col];
-            row = row == NO_ROW ? 0 : row;
-            const uint16_t* p = base + (uint64_t)row * (FULL ? DP : d);
+        for (int n = 0; n < NR; ++n)
 #pragma unroll
-            for (int c = 0; c < KS; ++c) kf[k][c] = *reinterpret_cast<const v4i*>(p + (FULL ? c * 4 + quad : min(c * 4 + quad, d / 8 - 1)) * 8);
+            for (int e = 0; e < KT / 4; ++e) sc[n][e / 4][e % 4] *= scale_log2;
+        if (!all) {
+#pragma unroll
+            for (int e = 0; e < KT / 4; ++e) {
+                const bool seen = sees[e / 8] >> quad * 4 & 1u << (e / 4 % 2 * 16 + e % 4);
+#pragma unroll
+                for (int n = 0; n < NR; ++n) sc[n][e / 4][e % 4] = seen ? sc[n][e / 4][e % 4] : -INFINITY;
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+            mx[n] = -INFINITY;
+#pragma unroll
+            for (int e = 0; e < KT / 16; ++e) mx[n] = fmaxf(fmaxf(fmaxf(mx[n], sc[n][e][0]), fmaxf(sc[n][e][1], sc[n][e][2])), sc[n][e][3]);
+            mx[n] = rows_max(mx[n]);
+            grown |= mx[n] > m[n] + 8.f;
+        }
+        if (__any(grown)) {
+#pragma unroll
+            for (int n = 0; n < NR; ++n) {
+                const float next = fmaxf(m[n], mx[n]);
+                rescale(n, m[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[n] - next));
+                m[n] = next;
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+            const float base = m[n] == -INFINITY ? 0.f : m[n];
+#pragma unroll
+            for (int j = 0; j < KT / 32; ++j) {
+                float p[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    p[e] = __builtin_amdgcn_exp2f(sc[n][j * 2 + e / 4][e % 4] - base);
+                    l[n] += p[e];
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    pf[n][0][j][e] = pack<BF16>(p[2 * e], p[2 * e + 1]);
+                    if constexpr (TERMS == 2)
+                        pf[n][1][j][e] = pack<BF16>(p[2 * e] - value_of<BF16>((uint32_t)pf[n][0][j][e] & 0xffffu), p[2 * e + 1] - value_of<BF16>((uint32_t)pf[n][0][j][e] >> 16));
+                }
+            }
         }
     }
-    __device__ __forceinline__ void load_v(const uint16_t* base, const uint32_t* rows, int d) {
-        const int lane = threadIdx.x % 64, at = (FULL ? lane % LPR : min(lane % LPR, d / 8 - 1)) * 8;
+    __device__ __forceinline__ void rescale(int n, float f) {
+        l[n] *= f;
 #pragma unroll
-        for (int j = 0; j < VI; ++j) {
-            uint32_t row = rows[j * RPI + lane / LPR];
-            row = row == NO_ROW ? 0 : row;
-            vr[j] = *reinterpret_cast<const v4i*>(base + (uint64_t)row * (FULL ? DP : d) + at);
+        for (int c = 0; c < CT; ++c) o[n][c] *= f;
+    }
+    __device__ __forceinline__ void add(const uint16_t* vs) {
+#pragma unroll
+        for (int j = 0; j < KT / 32; ++j)
+#pragma unroll
+            for (int c = 0; c < CT; ++c) {
+                const v4i vf = get_v(vs + j * 32 * VLD, c);
+#pragma unroll
+                for (int n = 0; n < NR; ++n)
+#pragma unroll
+                    for (int k = 0; k < TERMS; ++k) o[n][c] = mfma<BF16>(vf, pf[n][k][j], o[n][c]);
+            }
+    }
+};
+
+// The same with the wave's own keys: K from memory into registers, V through registers into the wave's LDS.
+template <bool BF16, int DP, int NR, int TERMS, bool FULL>
+struct own_keys : flash<BF16, DP, NR, 32, TERMS, FULL> {
+    typedef flash<BF16, DP, NR, 32, TERMS, FULL> base;
+    static constexpr int VI = DP / 16, LPR = DP / 8, RPI = 64 / LPR;   // pieces of V of a lane, lanes on a row, rows at a time
+    v4i kf[2][base::KS], vr[VI];
+    // Pieces behind the head dimension read another one, and count as 0.
+    __device__ __forceinline__ void load_k(const v4i* from, const uint32_t* rows, int d) {
+        const int col = threadIdx.x % 16, quad = threadIdx.x % 64 / 16;
+        if (FULL) from += quad;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const v4i* p = from + rows[k * 16 + col];
+#pragma unroll
+            for (int c = 0; c < base::KS; ++c) kf[k][c] = p[FULL ? c * 4 : min(c * 4 + quad, d / 8 - 1)];
         }
+    }
+    __device__ __forceinline__ void load_v(const v4i* from, const uint32_t* rows, int d) {
+        const int lane = threadIdx.x % 64;
+        from += FULL ? lane % LPR : min(lane % LPR, d / 8 - 1);
+#pragma unroll
+        for (int j = 0; j < VI; ++j) vr[j] = from[rows[j * RPI + lane / LPR]];
     }
     // V from registers into LDS; rows of keys that are not there become 0.
     __device__ __forceinline__ void put_v(uint16_t* vs, uint32_t there) {
@@ -178,22 +264,15 @@ struct flash {
             for (int j = 0; j < VI; ++j)
                 if (!(held & 1u << (j * RPI))) vr[j] = v4i{0, 0, 0, 0};
         }
-        uint16_t* to = vs + (lane / LPR) * VLD + lane % LPR * 8;
+        uint16_t* to = vs + (lane / LPR) * base::VLD + lane % LPR * 8;
 #pragma unroll
-        for (int j = 0; j < VI; ++j) *reinterpret_cast<v4i*>(to + j * RPI * VLD) = vr[j];
-    }
-    __device__ __forceinline__ v4i get_v(const uint16_t* vs, int c) const {
-        const int col = threadIdx.x % 16, quad = threadIdx.x % 64 / 16;
-        const uint16_t* from = vs + (quad * 4 + col / 4) * VLD + col % 4 * 4 + c * 16;
-        const v2i x = __builtin_bit_cast(v2i, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(from)));
-        const v2i y = __builtin_bit_cast(v2i, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(from + 16 * VLD)));
-        return v4i{x[0], x[1], y[0], y[1]};
+        for (int j = 0; j < VI; ++j) *reinterpret_cast<v4i*>(to + j * RPI * base::VLD) = vr[j];
     }
     __device__ __forceinline__ void scores(int d) {
         if constexpr (!FULL) {
             const int quad = threadIdx.x % 64 / 16;
 #pragma unroll
-            for (int c = 0; c < KS; ++c) {
+            for (int c = 0; c < base::KS; ++c) {
                 const int keep = (c * 4 + quad - d / 8) >> 31;
                 kf[0][c] &= keep;
                 kf[1][c] &= keep;
@@ -203,56 +282,10 @@ struct flash {
         for (int k = 0; k < 2; ++k)
 #pragma unroll
             for (int n = 0; n < NR; ++n) {
-                sc[n][k] = v4f{0.f, 0.f, 0.f, 0.f};
+                this->sc[n][k] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int c = 0; c < KS; ++c) sc[n][k] = mfma<BF16>(kf[k][c], qf[n][c], sc[n][k]);
+                for (int c = 0; c < base::KS; ++c) this->sc[n][k] = mfma<BF16>(kf[k][c], this->qf[n][c], this->sc[n][k]);
             }
-    }
-    // The weights of 32 keys for 16 rows; `sees`: which keys the lane's row sees.
-    __device__ __forceinline__ void weigh(int n, float scale_log2, uint32_t sees, bool all) {
-        const int quad = threadIdx.x % 64 / 16;
-        float p[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) p[e] = sc[n][e / 4][e % 4] * scale_log2;
-        if (!all) {
-            sees >>= quad * 4;
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (!(sees & 1u << (e / 4 * 16 + e % 4))) p[e] = -INFINITY;
-        }
-        const float mx = rows_max(fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])), fmaxf(fmaxf(p[4], p[5]), fmaxf(p[6], p[7]))));
-        if (__any(mx > m[n])) {
-            const float next = fmaxf(m[n], mx);
-            rescale(n, m[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[n] - next));
-            m[n] = next;
-        }
-        const float base = m[n] == -INFINITY ? 0.f : m[n];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            p[e] = __builtin_amdgcn_exp2f(p[e] - base);
-            l[n] += p[e];
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            pf[n][0][e] = pack<BF16>(p[2 * e], p[2 * e + 1]);
-            if constexpr (TERMS == 2)
-                pf[n][1][e] = pack<BF16>(p[2 * e] - value_of<BF16>((uint32_t)pf[n][0][e] & 0xffffu), p[2 * e + 1] - value_of<BF16>((uint32_t)pf[n][0][e] >> 16));
-        }
-    }
-    __device__ __forceinline__ void rescale(int n, float f) {
-        l[n] *= f;
-#pragma unroll
-        for (int c = 0; c < CT; ++c) o[n][c] *= f;
-    }
-    __device__ __forceinline__ void add(const uint16_t* vs) {
-#pragma unroll
-        for (int c = 0; c < CT; ++c) {
-            const v4i vf = get_v(vs, c);
-#pragma unroll
-            for (int n = 0; n < NR; ++n)
-#pragma unroll
-                for (int k = 0; k < TERMS; ++k) o[n][c] = mfma<BF16>(vf, pf[n][k], o[n][c]);
-        }
     }
 };
 
@@ -283,48 +316,89 @@ __device__ __forceinline__ void join_waves(F& f, int n, float* os, float (*top)[
     }
 }
 
-// Workgroup (part, tile of rows): the part's keys, pair by pair.
-template <bool BF16, int DP, int NR, bool FULL>
-__global__ __launch_bounds__(256, DP == 256 ? 1 : NR == 1 ? 3 : NR == 2 ? 2 : 1) void attend_context_kernel(attend_args a) {
-    constexpr int ROWS = 16 * NR;
-    typedef flash<BF16, DP, NR, 2, FULL> state;
-    __shared__ __align__(16) unsigned char pool[4 * 32 * state::VLD * 2];
-    __shared__ uint32_t listed[LISTED];
-    __shared__ float top[4][16], sum[4][16];
-    __shared__ int waves[4], where[2];
-    static_assert(4 * 16 * (DP + 4) * 4 <= sizeof(pool), "the waves' parts of the result fit their rows of V");
-
-    const int t = threadIdx.x, lane = t % 64, wave = uniform(t / 64);
-    // workgroups of the same part and different tiles read the same keys: 8 apart, they run behind the same L2
-    const int tile = (int)(blockIdx.x / 8) % a.tiles, part = (int)(blockIdx.x / 8) / a.tiles * 8 + (int)(blockIdx.x % 8);
-    int at = 0, end = 0, quota = 0;
-    for (int pass = a.B <= 256; pass < 2; ++pass) {
+// Where a workgroup's part of the line starts and ends, and the stream and the unit within it that it starts at.  Thread 0 of workgroup 0 and
+// its fellows leave the streams' places for the second kernel.
+__device__ __forceinline__ bool place_part(const attend_args& a, int part, int* waves, int* where, int* at, int* end) {
+    const int t = threadIdx.x, threads = blockDim.x;
+    int quota = 0;
+    for (int pass = a.B <= threads; pass < 2; ++pass) {
         int before = 0, all;
-        for (int base = 0; base < a.B; base += 256) {
+        for (int base = 0; base < a.B; base += threads) {
             const int i = base + t, n = i < a.B ? a.H * stream_of(a, i, blockIdx.x == 0).units : 0;
             const int start = before + block_before(n, waves, &all);
             before += all;
-            if (pass == 0 || a.B <= 256) {
+            if (pass == 0 || a.B <= threads) {
                 const int units = uniform(before);
                 quota = quota_of(a, units);
-                at = part * quota;
-                end = min(at + quota, units);
+                *at = part * quota;
+                *end = min(*at + quota, units);
             }
             if (pass) {
-                if (start <= at && at < start + n) where[0] = i, where[1] = at - start;
+                if (start <= *at && *at < start + n) where[0] = i, where[1] = *at - start;
                 if (blockIdx.x == 0 && i < a.B) a.starts[i] = start;
             }
         }
         if (blockIdx.x == 0 && t == 0) a.starts[a.B] = before;
     }
     __syncthreads();
-    if (at >= end || part >= a.parts) return;
+    return *at < *end && part < a.parts;
+}
+
+// Looks up where the rows of keys from * UNIT .. (from + n) * UNIT of a pair start in its layer's pool, in pieces of 16 bytes, and which
+// keys are there; one that is not reads row 0 and weighs nothing.
+__device__ __forceinline__ void list_keys(const attend_args& a, const stream& s, int b, int h, int from, int n, uint32_t* listed, uint32_t* held) {
+    const int lane = threadIdx.x % 64, inside = (1 << a.page_log2) - 1;
+    __syncthreads();
+    for (int x = threadIdx.x; x < n * UNIT; x += blockDim.x) {
+        uint32_t row = 0;
+        bool there = false;
+        int pos = from * UNIT + x;
+        if (pos < s.slots) {
+            if (a.sel) {
+                const bool by_page = a.unit == SWARM_SEL_PAGES;
+                const int e = a.sel[((int64_t)b * a.H + h) * a.n_sel + (by_page ? pos >> a.page_log2 : pos)];
+                pos = by_page ? e << a.page_log2 | (pos & inside) : e;
+                if (e < 0 || e >= (by_page ? a.cap : a.cap << a.page_log2)) {
+                    if (e != -1) atomicOr(a.flags, SWARM_DEV_BAD_ENTRY);
+                    pos = s.len;
+                }
+            }
+            if (pos < s.len) {
+                const int id = a.table[(int64_t)b * a.cap + (pos >> a.page_log2)];
+                if (id < 0 || id >= a.P) atomicOr(a.flags, SWARM_DEV_BAD_PAGE);
+                else there = true, row = (((uint32_t)id * a.H + h) << a.page_log2) + (pos & inside);
+            }
+        }
+        listed[x] = row * (uint32_t)(a.d / 8);
+        const uint64_t which = __ballot(there);
+        if (lane % 32 == 0) held[x / 32] = (uint32_t)(which >> lane);
+    }
+    __syncthreads();
+}
+
+// Workgroup (part, tile of up to 32 rows): the part's keys, pair by pair, each wave 32 keys of a unit and all rows.
+template <bool BF16, int DP, int NR, bool FULL>
+__global__ __launch_bounds__(256, DP == 256 ? 1 : NR == 1 ? 3 : 2) void attend_context_kernel(attend_args a) {
+    constexpr int ROWS = 16 * NR;
+    typedef own_keys<BF16, DP, NR, 2, FULL> state;
+    __shared__ __align__(16) unsigned char pool[4 * 32 * state::VLD * 2];
+    __shared__ uint32_t listed[LISTED], held[LISTED / 32];
+    __shared__ float top[4][16], sum[4][16];
+    __shared__ int waves[4], where[2];
+    static_assert(4 * 16 * (DP + 4) * 4 <= sizeof(pool), "the waves' parts of the result fit their rows of V");
+
+    const int wave = uniform(threadIdx.x / 64);
+    // workgroups of the same part and different tiles read the same keys: 8 apart, they run behind the same L2
+    const int tile = (int)(blockIdx.x / 8) % a.tiles, part = (int)(blockIdx.x / 8) / a.tiles * 8 + (int)(blockIdx.x % 8);
+    int at, end;
+    if (!place_part(a, part, waves, where, &at, &end)) return;
     int b = uniform(where[0]);
     const int offset = uniform(where[1]);
     stream s = stream_of(a, b, false);
     int h = offset / s.units, first = offset % s.units;
     uint16_t* vs = reinterpret_cast<uint16_t*>(pool) + wave * 32 * state::VLD;
     const uint32_t* mine = listed + wave * 32;
+    const v4i *kp = reinterpret_cast<const v4i*>(a.k), *vp = reinterpret_cast<const v4i*>(a.v);
     state f;
 
     for (;;) {
@@ -332,46 +406,21 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : NR == 1 ? 3 : NR == 2 ? 2 : 1)
         const int rows = min(s.drafted * a.G - tile * ROWS, ROWS);   // query rows here
         if (rows > 0) {
             f.start(a, b, h, tile * ROWS, s.drafted);
-            // pieces of the pair's keys whose rows are looked up together
             for (int u0 = first; u0 < last; u0 += LISTED / UNIT) {
                 const int n = min(last - u0, LISTED / UNIT);
-                __syncthreads();
-                for (int x = t; x < n * UNIT; x += 256) {
-                    uint32_t row = NO_ROW;
-                    int pos = u0 * UNIT + x;
-                    if (pos < s.slots) {
-                        const int in = pos & ((1 << a.page_log2) - 1);
-                        if (a.sel) {
-                            const bool by_page = a.unit == SWARM_SEL_PAGES;
-                            const int e = a.sel[((int64_t)b * a.H + h) * a.n_sel + (by_page ? pos >> a.page_log2 : pos)];
-                            pos = by_page ? e << a.page_log2 | in : e;
-                            if (e < 0 || e >= (by_page ? a.cap : a.cap << a.page_log2)) {
-                                if (e != -1) atomicOr(a.flags, SWARM_DEV_BAD_ENTRY);
-                                pos = s.len;
-                            }
-                        }
-                        if (pos < s.len) {
-                            const int id = a.table[(int64_t)b * a.cap + (pos >> a.page_log2)];
-                            if (id < 0 || id >= a.P) atomicOr(a.flags, SWARM_DEV_BAD_PAGE);
-                            else row = (((uint32_t)id * a.H + h) << a.page_log2) + (pos & ((1 << a.page_log2) - 1));
-                        }
-                    }
-                    listed[x] = row;
-                }
-                __syncthreads();
+                list_keys(a, s, b, h, u0, n, listed, held);
                 // K and V of the next tile are on their way while one is worked on: V into registers as soon as LDS has taken the last
                 // one's, K as soon as its products are issued
-                f.load_v(a.v, mine, a.d);
-                f.load_k(a.k, mine, a.d);
+                f.load_v(vp, mine, a.d);
+                f.load_k(kp, mine, a.d);
                 for (int u = 0; u < n; ++u) {
-                    const uint32_t there = (uint32_t)__ballot(mine[u * UNIT + lane % 32] != NO_ROW);
+                    const uint32_t there = (uint32_t)uniform((int)held[u * 4 + wave]);
+                    const int next = min(u + 1, n - 1) * UNIT;
                     f.put_v(vs, there);
-                    if (u + 1 < n) f.load_v(a.v, mine + (u + 1) * UNIT, a.d);
+                    f.load_v(vp, mine + next, a.d);
                     f.scores(a.d);
-                    if (u + 1 < n) f.load_k(a.k, mine + (u + 1) * UNIT, a.d);
-                    const bool all = there == ~0u;
-#pragma unroll
-                    for (int r = 0; r < NR; ++r) f.weigh(r, a.scale_log2, there, all);
+                    f.load_k(kp, mine + next, a.d);
+                    f.weigh(a.scale_log2, &there, there == ~0u);
                     f.add(vs);
                 }
             }
@@ -396,10 +445,114 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : NR == 1 ? 3 : NR == 2 ? 2 : 1)
     }
 }
 
+// The same for many rows: W waves of 32 rows each share tiles of KT keys in LDS, K and V, two of them: while one is worked on,
+// the next comes into registers, and from there into the other's place.
+template <bool BF16, int DP, int W, bool FULL>
+__global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void attend_wide_kernel(attend_args a) {
+    constexpr int ROWS = 32 * W, KT = DP == 256 || W == 2 ? 32 : 64, THREADS = 64 * W;
+    typedef flash<BF16, DP, 2, KT, 2, FULL> state;
+    constexpr int KLD = DP + 8, VLD = state::VLD;     // LDS rows: 16 rows' pieces of 16 bytes meet no bank twice
+    constexpr int LPR = DP / 8, PIECES = KT * LPR, MINE = (PIECES + THREADS - 1) / THREADS;
+    __shared__ __align__(16) uint16_t ks[2][KT * KLD], vs[2][KT * VLD];
+    __shared__ uint32_t listed[LISTED], held[LISTED / 32];
+    __shared__ int waves[W], where[2];
+
+    const int t = threadIdx.x, lane = t % 64, col = lane % 16, quad = lane / 16, wave = uniform(t / 64);
+    const int tile = (int)(blockIdx.x / 8) % a.tiles, part = (int)(blockIdx.x / 8) / a.tiles * 8 + (int)(blockIdx.x % 8);
+    int at, end;
+    if (!place_part(a, part, waves, where, &at, &end)) return;
+    int b = uniform(where[0]);
+    const int offset = uniform(where[1]);
+    stream s = stream_of(a, b, false);
+    int h = offset / s.units, first = offset % s.units;
+    const v4i *kp = reinterpret_cast<const v4i*>(a.k), *vp = reinterpret_cast<const v4i*>(a.v);
+    state f;
+    v4i kr[MINE], vr[MINE];
+
+    for (;;) {
+        const int last = min(s.units, first + (end - at));
+        const int rows = min(s.drafted * a.G - tile * ROWS, ROWS);   // query rows here
+        if (rows > 0) {
+            f.start(a, b, h, tile * ROWS + wave * 32, s.drafted);
+            for (int u0 = first; u0 < last; u0 += LISTED / UNIT) {
+                const int n = min(last - u0, LISTED / UNIT) * (UNIT / KT);
+                list_keys(a, s, b, h, u0, n / (UNIT / KT), listed, held);
+                auto load = [&](int u) {
+#pragma unroll
+                    for (int j = 0; j < MINE; ++j) {
+                        const int x = min(t + j * THREADS, PIECES - 1), piece = x % LPR;
+                        const uint32_t row = listed[u * KT + x / LPR] + (FULL ? piece : min(piece, a.d / 8 - 1));
+                        kr[j] = kp[row];
+                        vr[j] = vp[row];
+                    }
+                };
+                // pieces behind the head dimension count as 0 on K's side; rows of keys that are not there do on V's
+                auto put = [&](int u) {
+#pragma unroll
+                    for (int j = 0; j < MINE; ++j) {
+                        const int x = t + j * THREADS, key = x / LPR, piece = x % LPR;
+                        if (PIECES % THREADS == 0 || x < PIECES) {
+                            const bool there = held[u * (KT / 32) + key / 32] >> (key % 32) & 1u;
+                            *reinterpret_cast<v4i*>(&ks[u & 1][key * KLD + piece * 8]) = FULL || piece < a.d / 8 ? kr[j] : v4i{0, 0, 0, 0};
+                            *reinterpret_cast<v4i*>(&vs[u & 1][key * VLD + piece * 8]) = there ? vr[j] : v4i{0, 0, 0, 0};
+                        }
+                    }
+                };
+                load(0);
+                put(0);
+                __syncthreads();
+                for (int u = 0; u < n; ++u) {
+                    load(min(u + 1, n - 1));
+                    uint32_t there[KT / 32], every = ~0u;
+#pragma unroll
+                    for (int j = 0; j < KT / 32; ++j) {
+                        there[j] = (uint32_t)uniform((int)held[u * (KT / 32) + j]);
+                        every &= there[j];
+                    }
+                    const uint16_t* kl = &ks[u & 1][col * KLD + quad * 8];
+#pragma unroll
+                    for (int k = 0; k < KT / 16; ++k) {
+                        f.sc[0][k] = f.sc[1][k] = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int c = 0; c < state::KS; ++c) {
+                            const v4i kf = *reinterpret_cast<const v4i*>(kl + k * 16 * KLD + c * 32);
+                            f.sc[0][k] = mfma<BF16>(kf, f.qf[0][c], f.sc[0][k]);
+                            f.sc[1][k] = mfma<BF16>(kf, f.qf[1][c], f.sc[1][k]);
+                        }
+                    }
+                    f.weigh(a.scale_log2, there, every == ~0u);
+                    f.add(vs[u & 1]);
+                    if (u + 1 < n) put(u + 1);
+                    __syncthreads();
+                }
+            }
+            const int64_t slot = (((int64_t)b * a.H + h + part) * a.tiles + tile) * ROWS;
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const int row = wave * 32 + r * 16 + col;
+                const float l = rows_sum(f.l[r]);
+                if (row < rows) {
+#pragma unroll
+                    for (int c = 0; c < state::CT; ++c) *reinterpret_cast<v4f*>(a.part_o + (slot + row) * DP + c * 16 + quad * 4) = f.o[r][c];
+                    if (quad == 0) a.part_ml[(slot + row) * 2] = f.m[r], a.part_ml[(slot + row) * 2 + 1] = l;
+                }
+            }
+        }
+        at += last - first;
+        if (at >= end) break;
+        first = 0;
+        if (++h == a.H) {
+            h = 0;
+            do s = stream_of(a, ++b, false);
+            while (s.units == 0);
+        }
+    }
+}
+
 // Workgroup (pair, 16 rows): the drafted tokens, the parts of the context, the end.
 template <bool BF16, int DP, bool FULL>
 __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attend_finish_kernel(attend_args a) {
-    typedef flash<BF16, DP, 1, 2, FULL> state;
+    typedef own_keys<BF16, DP, 1, 2, FULL> state;
     constexpr uint32_t EXP = BF16 ? 0x7f80u : 0x7c00u;
     __shared__ __align__(16) unsigned char pool[4 * 32 * state::VLD * 2];
     __shared__ uint32_t listed[256];
@@ -413,13 +566,14 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attend_finish_kernel(a
     state f;
     f.start(a, b, h, row0, s.drafted);
     if (a.k_new) {
-        listed[t] = t < s.drafted ? ((uint32_t)b * a.T + t) * a.H + h : NO_ROW;
+        const v4i *kp = reinterpret_cast<const v4i*>(a.k_new), *vp = reinterpret_cast<const v4i*>(a.v_new);
+        listed[t] = (((uint32_t)b * a.T + min(t, s.drafted - 1)) * a.H + h) * (uint32_t)(a.d / 8);
         __syncthreads();
         const int token = token_of(a, row0 + col);
         for (int j0 = wave * 32; j0 < s.drafted; j0 += UNIT) {
             const uint32_t there = s.drafted - j0 >= 32 ? ~0u : (1u << (s.drafted - j0)) - 1u;
-            f.load_k(a.k_new, listed + j0, a.d);
-            f.load_v(a.v_new, listed + j0, a.d);
+            f.load_k(kp, listed + j0, a.d);
+            f.load_v(vp, listed + j0, a.d);
             // Not every row sees these: values that are not numbers stand apart.
             bool odd = false;
 #pragma unroll
@@ -438,7 +592,8 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attend_finish_kernel(a
                 if (a.mask) word = a.mask[((int64_t)b * a.T + token) * ((a.T + 31) / 32) + j0 / 32];
                 else word = token - j0 >= 31 ? ~0u : token < j0 ? 0u : (2u << (token - j0)) - 1u;
             }
-            f.weigh(0, a.scale_log2, word & there, false);
+            const uint32_t sees = word & there;
+            f.weigh(a.scale_log2, &sees, false);
             f.add(vs);
             if (__any(odd)) {
                 // One drafted token at a time: its values that are not numbers alone in LDS, and only the rows that weigh it take the
@@ -446,7 +601,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attend_finish_kernel(a
 #pragma unroll 1
                 for (int j = 0; j < 32; ++j) {
                     if (!(there >> j & 1u)) continue;
-                    f.load_v(a.v_new, listed + j0, a.d);
+                    f.load_v(vp, listed + j0, a.d);
 #pragma unroll
                     for (int i = 0; i < state::VI; ++i)
 #pragma unroll
@@ -460,7 +615,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attend_finish_kernel(a
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
                         if (e / 4 * 16 + quad * 4 + e % 4 == j) {
-                            any = (uint32_t)f.pf[0][0][e / 2] & (e % 2 ? 0xffff0000u : 0xffffu);
+                            any = (uint32_t)f.pf[0][0][0][e / 2] & (e % 2 ? 0xffff0000u : 0xffffu);
                             alone[e / 2] = (int)any;
                         }
                     const bool takes = rows_max(any ? 1.f : 0.f) > 0.f;
@@ -480,20 +635,24 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attend_finish_kernel(a
         // this row in the tiles of the first kernel
         const int tile = row0 / a.rows, in = row0 % a.rows + min(col, rows - 1);
         auto slot = [&](int p) { return (((int64_t)b * a.H + h + p) * a.tiles + tile) * a.rows + in; };
+        // Every other part's maximum first, then their sums, several parts on their way at a time.  A part without keys left zeros.
         float big = f.m[0];
+#pragma unroll 4
         for (int p = p0 + wave; p <= p1; p += 4) big = fmaxf(big, a.part_ml[slot(p) * 2]);
         if (f.m[0] != -INFINITY) f.rescale(0, __builtin_amdgcn_exp2f(f.m[0] - big));
         f.m[0] = big;
-#pragma unroll 2
+#pragma unroll 4
         for (int p = p0 + wave; p <= p1; p += 4) {
-            const float m = a.part_ml[slot(p) * 2], z = a.part_ml[slot(p) * 2 + 1], w = m == -INFINITY ? 0.f * z : __builtin_amdgcn_exp2f(m - big);
-            if (quad == 0) f.l[0] += w * z;
-            const float* part = a.part_o + slot(p) * DP + quad * 4;
+            const int64_t at = slot(p);
+            const float m = a.part_ml[at * 2], z = a.part_ml[at * 2 + 1];
+            const float* part = a.part_o + at * DP + quad * 4;
+            v4f x[state::CT];
 #pragma unroll
-            for (int c = 0; c < state::CT; ++c) {
-                const v4f x = *reinterpret_cast<const v4f*>(part + c * 16);
-                if (w > 0.f || w != w) f.o[0][c] += w * x;
-            }
+            for (int c = 0; c < state::CT; ++c) x[c] = *reinterpret_cast<const v4f*>(part + c * 16);
+            const float w = m == -INFINITY ? 0.f * z : __builtin_amdgcn_exp2f(m - big);
+            if (quad == 0) f.l[0] += w * z;
+#pragma unroll
+            for (int c = 0; c < state::CT; ++c) f.o[0][c] += w * x[c];
         }
     }
     join_waves<DP>(f, 0, reinterpret_cast<float*>(pool), top, sum, [&](int row, int c, v4f y, float m, float z) {
@@ -512,10 +671,10 @@ void launch_attend(const attend_args& a, hipStream_t stream) {
     const dim3 grid((unsigned)((a.parts + 7) / 8 * 8 * a.tiles)), block(256);
     if (a.rows == 16) hipLaunchKernelGGL((attend_context_kernel<BF16, DP, 1, FULL>), grid, block, 0, stream, a);
     else if (a.rows == 32) hipLaunchKernelGGL((attend_context_kernel<BF16, DP, 2, FULL>), grid, block, 0, stream, a);
-    else if constexpr (DP <= 128) {
-        if (a.rows == 48) hipLaunchKernelGGL((attend_context_kernel<BF16, DP, 3, FULL>), grid, block, 0, stream, a);
-        else hipLaunchKernelGGL((attend_context_kernel<BF16, DP, 4, FULL>), grid, block, 0, stream, a);
-    }
+    else if (a.rows == 64) hipLaunchKernelGGL((attend_wide_kernel<BF16, DP, 2, FULL>), grid, dim3(128), 0, stream, a);
+    else if (a.rows == 128) hipLaunchKernelGGL((attend_wide_kernel<BF16, DP, 4, FULL>), grid, block, 0, stream, a);
+    else if (a.rows == 192) hipLaunchKernelGGL((attend_wide_kernel<BF16, DP, 6, FULL>), grid, dim3(384), 0, stream, a);
+    else hipLaunchKernelGGL((attend_wide_kernel<BF16, DP, 8, FULL>), grid, dim3(512), 0, stream, a);
     hipLaunchKernelGGL((attend_finish_kernel<BF16, DP, FULL>), dim3((unsigned)(a.B * a.H), (unsigned)((a.T * a.G + 15) / 16)), block, 0, stream, a);
 }
 
@@ -542,8 +701,8 @@ extern "C" swarm_status swarm_tree_attend(swarm_ctx* ctx, const swarm_cache* cac
     if (G < 1 || G > 1024) SWARM_REJECT(ctx, "tree_attend: G=%d outside [1,1024]", G);
     const int64_t rows = (int64_t)B * T * cache->H * G;
     if (rows > ((int64_t)1 << 30)) SWARM_REJECT(ctx, "tree_attend: B*T*H*G above 2^30");
-    if ((int64_t)cache->P * cache->H * cache->page >= UINT32_MAX || (int64_t)B * T * cache->H >= UINT32_MAX)
-        SWARM_REJECT(ctx, "tree_attend: P*H*page or B*T*H above 2^32 - 2");
+    if ((int64_t)cache->P * cache->H * cache->page * (cache->d / 8) > UINT32_MAX || (int64_t)B * T * cache->H * (cache->d / 8) > UINT32_MAX)
+        SWARM_REJECT(ctx, "tree_attend: a layer of the pool, or k_new, of 64 GiB or more");
     if (sel && (n_sel < 1 || n_sel > (1 << 30) / (unit == SWARM_SEL_PAGES ? cache->page : 1)))
         SWARM_REJECT(ctx, "tree_attend: n_sel=%d below 1, or above 2^30 tokens", n_sel);
     if (sel && unit != SWARM_SEL_PAGES && unit != SWARM_SEL_TOKENS) SWARM_REJECT(ctx, "tree_attend: unknown unit %d", unit);
@@ -560,15 +719,21 @@ extern "C" swarm_status swarm_tree_attend(swarm_ctx* ctx, const swarm_cache* cac
     if (swarm_overlap(outs, 2, ins, 10)) SWARM_REJECT(ctx, "tree_attend: out or lse overlaps an input, or the other");
 
     attend_args a{};
-    // Row tiles of at most 64 rows (32 of wide heads: the sums must stay in registers), as even as multiples of 16 allow: a tile pays for all its rows.
-    const int M = T * G, DP = cache->d <= 64 ? 64 : cache->d <= 128 ? 128 : 256, most = DP > 128 ? 32 : 64;
-    a.tiles = (M + most - 1) / most;
-    a.rows = (M + 16 * a.tiles - 1) / (16 * a.tiles) * 16;
+    // Up to 32 rows go to the kernel whose waves have keys of their own, more to the one whose waves share them, 32 rows a wave: as few tiles
+    // of rows as 8 waves allow, and in each as few waves as the rows need.
+    const int M = T * G, DP = cache->d <= 64 ? 64 : cache->d <= 128 ? 128 : 256;
+    if (M <= 32) {
+        a.tiles = 1;
+        a.rows = (M + 15) / 16 * 16;
+    } else {
+        a.tiles = (M + 255) / 256;
+        a.rows = (M + 64 * a.tiles - 1) / (64 * a.tiles) * 64;
+    }
     // as many parts as workgroups are resident at once, and no more than there can be units
     const int64_t slots = !sel ? (int64_t)cache->cap * cache->page : unit == SWARM_SEL_PAGES ? (int64_t)n_sel * cache->page : n_sel;
     const int64_t units = (int64_t)B * cache->H * ((slots + UNIT - 1) / UNIT);
     if (units > INT32_MAX - 65536) SWARM_REJECT(ctx, "tree_attend: contexts of up to %lld times 128 keys, above 2^31", (long long)units);
-    const int resident = 256 * (DP > 128 ? 1 : a.rows == 16 ? 3 : a.rows == 32 ? 2 : 1), want = a.tiles < resident ? resident / a.tiles : 1;
+    const int resident = 256 * (DP > 128 ? 1 : a.rows == 16 ? 3 : a.rows <= 128 ? 2 : 1), want = a.tiles < resident ? resident / a.tiles : 1;
     a.parts = (int)(units < want ? units : want);
     const size_t heads = (4 * ((size_t)B + 1) + 15) / 16 * 16, left = ((size_t)B * cache->H + a.parts) * a.tiles * a.rows;
     st = swarm_scratch(ctx, &ctx->attend, &ctx->attend_bytes, heads + left * (DP + 2) * 4);
