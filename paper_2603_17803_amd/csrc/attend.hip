@@ -149,6 +149,22 @@ struct flash {
             for (int c = 0; c < CT; ++c) o[n][c] = v4f{0.f, 0.f, 0.f, 0.f};
         }
     }
+    // q . k of KT keys whose rows stand in LDS.
+    template <int KLD>
+    __device__ __forceinline__ void scores(const uint16_t* ks) {
+        const int col = threadIdx.x % 16, quad = threadIdx.x % 64 / 16;
+#pragma unroll
+        for (int k = 0; k < KT / 16; ++k) {
+#pragma unroll
+            for (int n = 0; n < NR; ++n) sc[n][k] = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < KS; ++c) {
+                const v4i kf = *reinterpret_cast<const v4i*>(ks + (k * 16 + col) * KLD + c * 32 + quad * 8);
+#pragma unroll
+                for (int n = 0; n < NR; ++n) sc[n][k] = mfma<BF16>(kf, qf[n][c], sc[n][k]);
+            }
+        }
+    }
     // V^T of 16 channels and 32 keys, as the operand of the second product: elements 0..3 and 4..7 of lane l are keys 4 (l / 16) + 0..3 and
     // 16 more.
     static __device__ __forceinline__ v4i get_v(const uint16_t* vs, int c) {
@@ -232,31 +248,32 @@ struct flash {
     }
 };
 
-// The same with the wave's own keys: K from memory into registers, V through registers into the wave's LDS.
+// The same with the wave's own keys: K and V through registers into the wave's LDS, one after the other in the same place.  Whole rows
+// come from memory at a time (as the operand of the first product K would come in 64 bytes of 16 rows).
 template <bool BF16, int DP, int NR, int TERMS, bool FULL>
 struct own_keys : flash<BF16, DP, NR, 32, TERMS, FULL> {
     typedef flash<BF16, DP, NR, 32, TERMS, FULL> base;
-    static constexpr int VI = DP / 16, LPR = DP / 8, RPI = 64 / LPR;   // pieces of V of a lane, lanes on a row, rows at a time
-    v4i kf[2][base::KS], vr[VI];
-    // Pieces behind the head dimension read another one, and count as 0.
-    __device__ __forceinline__ void load_k(const v4i* from, const uint32_t* rows, int d) {
-        const int col = threadIdx.x % 16, quad = threadIdx.x % 64 / 16;
-        if (FULL) from += quad;
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const v4i* p = from + rows[k * 16 + col];
-#pragma unroll
-            for (int c = 0; c < base::KS; ++c) kf[k][c] = p[FULL ? c * 4 : min(c * 4 + quad, d / 8 - 1)];
-        }
-    }
-    __device__ __forceinline__ void load_v(const v4i* from, const uint32_t* rows, int d) {
+    static constexpr int VI = DP / 16, LPR = DP / 8, RPI = 64 / LPR;   // pieces of a lane, lanes on a row, rows at a time
+    static constexpr int KLD = DP + 8, VLD = base::VLD;                // LDS rows in elements: 16 rows' pieces of 16 bytes meet no bank twice
+    v4i kr[VI], vr[VI];
+    // Pieces behind the head dimension read another one; on K's side they then count as 0.
+    static __device__ __forceinline__ void load(v4i (&r)[VI], const v4i* from, const uint32_t* rows, int d) {
         const int lane = threadIdx.x % 64;
         from += FULL ? lane % LPR : min(lane % LPR, d / 8 - 1);
 #pragma unroll
-        for (int j = 0; j < VI; ++j) vr[j] = from[rows[j * RPI + lane / LPR]];
+        for (int j = 0; j < VI; ++j) r[j] = __builtin_nontemporal_load(from + rows[j * RPI + lane / LPR]);
     }
-    // V from registers into LDS; rows of keys that are not there become 0.
-    __device__ __forceinline__ void put_v(uint16_t* vs, uint32_t there) {
+    __device__ __forceinline__ void put_k(uint16_t* lds, int d) {
+        const int lane = threadIdx.x % 64;
+        uint16_t* to = lds + (lane / LPR) * KLD + lane % LPR * 8;
+#pragma unroll
+        for (int j = 0; j < VI; ++j) {
+            if (!FULL) kr[j] &= (lane % LPR - d / 8) >> 31;
+            *reinterpret_cast<v4i*>(to + j * RPI * KLD) = kr[j];
+        }
+    }
+    // Rows of keys that are not there become 0.
+    __device__ __forceinline__ void put_v(uint16_t* lds, uint32_t there) {
         const int lane = threadIdx.x % 64;
         if (there != ~0u) {
             const uint32_t held = there >> (lane / LPR);
@@ -264,28 +281,9 @@ struct own_keys : flash<BF16, DP, NR, 32, TERMS, FULL> {
             for (int j = 0; j < VI; ++j)
                 if (!(held & 1u << (j * RPI))) vr[j] = v4i{0, 0, 0, 0};
         }
-        uint16_t* to = vs + (lane / LPR) * base::VLD + lane % LPR * 8;
+        uint16_t* to = lds + (lane / LPR) * VLD + lane % LPR * 8;
 #pragma unroll
-        for (int j = 0; j < VI; ++j) *reinterpret_cast<v4i*>(to + j * RPI * base::VLD) = vr[j];
-    }
-    __device__ __forceinline__ void scores(int d) {
-        if constexpr (!FULL) {
-            const int quad = threadIdx.x % 64 / 16;
-#pragma unroll
-            for (int c = 0; c < base::KS; ++c) {
-                const int keep = (c * 4 + quad - d / 8) >> 31;
-                kf[0][c] &= keep;
-                kf[1][c] &= keep;
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-            for (int n = 0; n < NR; ++n) {
-                this->sc[n][k] = v4f{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int c = 0; c < base::KS; ++c) this->sc[n][k] = mfma<BF16>(kf[k][c], this->qf[n][c], this->sc[n][k]);
-            }
+        for (int j = 0; j < VI; ++j) *reinterpret_cast<v4i*>(to + j * RPI * VLD) = vr[j];
     }
 };
 
@@ -378,7 +376,7 @@ __device__ __forceinline__ void list_keys(const attend_args& a, const stream& s,
 
 // Workgroup (part, tile of up to 32 rows): the part's keys, pair by pair, each wave 32 keys of a unit and all rows.
 template <bool BF16, int DP, int NR, bool FULL>
-__global__ __launch_bounds__(256, DP == 256 ? 1 : NR == 1 ? 3 : 2) void attend_context_kernel(attend_args a) {
+__global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attend_context_kernel(attend_args a) {
     constexpr int ROWS = 16 * NR;
     typedef own_keys<BF16, DP, NR, 2, FULL> state;
     __shared__ __align__(16) unsigned char pool[4 * 32 * state::VLD * 2];
@@ -409,17 +407,18 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : NR == 1 ? 3 : 2) void attend_c
             for (int u0 = first; u0 < last; u0 += LISTED / UNIT) {
                 const int n = min(last - u0, LISTED / UNIT);
                 list_keys(a, s, b, h, u0, n, listed, held);
-                // K and V of the next tile are on their way while one is worked on: V into registers as soon as LDS has taken the last
-                // one's, K as soon as its products are issued
-                f.load_v(vp, mine, a.d);
-                f.load_k(kp, mine, a.d);
+                // K and V of the next tile are on their way while one is worked on: into registers as soon as LDS has taken the last one's
+                f.load(f.kr, kp, mine, a.d);
+                __builtin_amdgcn_sched_barrier(0);   // K's loads stay older than V's, as in the loop: whoever waits for K then need not wait for V
+                f.load(f.vr, vp, mine, a.d);
                 for (int u = 0; u < n; ++u) {
                     const uint32_t there = (uint32_t)uniform((int)held[u * 4 + wave]);
                     const int next = min(u + 1, n - 1) * UNIT;
+                    f.put_k(vs, a.d);
+                    f.load(f.kr, kp, mine + next, a.d);
+                    f.template scores<state::KLD>(vs);
                     f.put_v(vs, there);
-                    f.load_v(vp, mine + next, a.d);
-                    f.scores(a.d);
-                    f.load_k(kp, mine + next, a.d);
+                    f.load(f.vr, vp, mine + next, a.d);
                     f.weigh(a.scale_log2, &there, there == ~0u);
                     f.add(vs);
                 }
@@ -509,17 +508,7 @@ __global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void attend_wide_kernel(
                         there[j] = (uint32_t)uniform((int)held[u * (KT / 32) + j]);
                         every &= there[j];
                     }
-                    const uint16_t* kl = &ks[u & 1][col * KLD + quad * 8];
-#pragma unroll
-                    for (int k = 0; k < KT / 16; ++k) {
-                        f.sc[0][k] = f.sc[1][k] = v4f{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                        for (int c = 0; c < state::KS; ++c) {
-                            const v4i kf = *reinterpret_cast<const v4i*>(kl + k * 16 * KLD + c * 32);
-                            f.sc[0][k] = mfma<BF16>(kf, f.qf[0][c], f.sc[0][k]);
-                            f.sc[1][k] = mfma<BF16>(kf, f.qf[1][c], f.sc[1][k]);
-                        }
-                    }
+                    f.template scores<KLD>(ks[u & 1]);
                     f.weigh(a.scale_log2, there, every == ~0u);
                     f.add(vs[u & 1]);
                     if (u + 1 < n) put(u + 1);
@@ -572,8 +561,10 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attend_finish_kernel(a
         const int token = token_of(a, row0 + col);
         for (int j0 = wave * 32; j0 < s.drafted; j0 += UNIT) {
             const uint32_t there = s.drafted - j0 >= 32 ? ~0u : (1u << (s.drafted - j0)) - 1u;
-            f.load_k(kp, listed + j0, a.d);
-            f.load_v(vp, listed + j0, a.d);
+            f.load(f.kr, kp, listed + j0, a.d);
+            f.load(f.vr, vp, listed + j0, a.d);
+            f.put_k(vs, a.d);
+            f.template scores<state::KLD>(vs);
             // Not every row sees these: values that are not numbers stand apart.
             bool odd = false;
 #pragma unroll
@@ -586,7 +577,6 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attend_finish_kernel(a
                     f.vr[j][e] = (int)x;
                 }
             f.put_v(vs, there);
-            f.scores(a.d);
             uint32_t word = 0;
             if (token < s.drafted) {
                 if (a.mask) word = a.mask[((int64_t)b * a.T + token) * ((a.T + 31) / 32) + j0 / 32];
@@ -601,7 +591,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attend_finish_kernel(a
 #pragma unroll 1
                 for (int j = 0; j < 32; ++j) {
                     if (!(there >> j & 1u)) continue;
-                    f.load_v(vp, listed + j0, a.d);
+                    f.load(f.vr, vp, listed + j0, a.d);
 #pragma unroll
                     for (int i = 0; i < state::VI; ++i)
 #pragma unroll
@@ -733,7 +723,7 @@ extern "C" swarm_status swarm_tree_attend(swarm_ctx* ctx, const swarm_cache* cac
     const int64_t slots = !sel ? (int64_t)cache->cap * cache->page : unit == SWARM_SEL_PAGES ? (int64_t)n_sel * cache->page : n_sel;
     const int64_t units = (int64_t)B * cache->H * ((slots + UNIT - 1) / UNIT);
     if (units > INT32_MAX - 65536) SWARM_REJECT(ctx, "tree_attend: contexts of up to %lld times 128 keys, above 2^31", (long long)units);
-    const int resident = 256 * (DP > 128 ? 1 : a.rows == 16 ? 3 : a.rows <= 128 ? 2 : 1), want = a.tiles < resident ? resident / a.tiles : 1;
+    const int resident = 256 * (DP > 128 ? 1 : a.rows <= 128 ? 2 : 1), want = a.tiles < resident ? resident / a.tiles : 1;
     a.parts = (int)(units < want ? units : want);
     const size_t heads = (4 * ((size_t)B + 1) + 15) / 16 * 16, left = ((size_t)B * cache->H + a.parts) * a.tiles * a.rows;
     st = swarm_scratch(ctx, &ctx->attend, &ctx->attend_bytes, heads + left * (DP + 2) * 4);
