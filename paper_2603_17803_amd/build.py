@@ -15,8 +15,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libswarm.so")
 OBJ_DIR = os.path.join(HERE, "_build")
 SOURCES = ["api.hip", "score.hip", "select.hip", "coact.hip", "coact_rows.hip", "mapper.hip", "density.hip", "window.hip", "retrieval.hip",
-           "calib.hip", "noalloc.hip", "attend.hip", "pages.hip", "beam.hip"]
-HEADERS = ["common.h", "wave_ops.h", "select_core.h"]
+           "calib.hip", "noalloc.hip", "attend.hip", "attend_fp16.hip", "pages.hip", "beam.hip"]
+HEADERS = ["common.h", "wave_ops.h", "select_core.h", "attend_core.h"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          # the fully unrolled epilogues of the co-activation kernel exceed the default budget of "#pragma unroll";

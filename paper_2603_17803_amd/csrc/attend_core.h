@@ -1,0 +1,725 @@
+// Attention of drafted tokens over a paged cache.
+//
+// The T*G query rows that a KV head's group has (drafted token i, query head g: row i*G + g) share every key and value, so a
+// workgroup takes up to 64 of them and streams the keys past: per 16 rows, S^T = K Q^T on the 16x16x32 matrix instruction (keys are
+// the rows of its result, query rows its columns), the softmax's running maximum and sum a lane per query row, O^T += V^T P^T on the
+// same instruction.  A lane's eight weights of 32 keys are, as they come out of the first product, one operand of the
+// second; V^T's operand is read out of LDS by the transposing read.  K goes straight from memory into registers.
+//
+// Two kernels.  The first takes the contexts: the 128-key units of all (stream, head) pairs stand in one line, which is cut into equal parts, one
+// for each workgroup, whatever the streams' lengths are.  The four waves of a workgroup each take 32 keys of a unit, all rows, and meet only
+// where a pair ends: no barrier in the loop.  What a part finds for a pair stays in scratch (fp32, unnormalised).  The second takes
+// 16 rows of a pair, works the drafted tokens in under their masks, joins the parts, divides and rounds once.
+#include <math.h>
+
+#include "common.h"
+
+struct attend_args {
+    const uint16_t *k, *v, *q, *k_new, *v_new;   // k, v: the layer's part of the pool
+    const int32_t *table, *len, *n_new, *sel;
+    const uint32_t* mask;
+    uint16_t* out;
+    float* lse;
+    int32_t* starts;                             // [B + 1]: where each stream's units start in the line, and their number
+    float* part_o;                               // [slots][rows of a tile][DP]: sums of weighted values
+    float* part_ml;                              // [slots][rows of a tile][2]: maximum (in units of ln 2) and sum of weights
+    uint32_t* flags;
+    int P, H, page_log2, d, cap, B, T, G, n_sel, unit;
+    int parts, tiles, rows;                      // parts of the line; tiles of a pair's rows, rows of a tile
+    uint32_t per_g;                              // ceil(2^32 / G)
+    float scale_log2;
+};
+
+// Head dimension that the kernels work with: the next of five.
+inline int attend_width(int d) { return d <= 64 ? 64 : d <= 96 ? 96 : d <= 128 ? 128 : d <= 192 ? 192 : 256; }
+constexpr int attend_wave_rows(int DP) { return DP > 128 ? 16 : 32; }   // rows of a wave of the kernel for many rows: what its sums leave room for in half of the register file
+constexpr int ATTEND_UNIT = 128;                                       // keys of a unit of the line
+
+void launch_attend_bf16(const attend_args& a, hipStream_t stream);
+void launch_attend_fp16(const attend_args& a, hipStream_t stream);
+
+namespace {
+
+typedef int v4i __attribute__((ext_vector_type(4)));
+typedef int v2i __attribute__((ext_vector_type(2)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
+typedef _Float16 hf8 __attribute__((ext_vector_type(8)));
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) v4s lds_v4s;
+
+constexpr int UNIT = ATTEND_UNIT;                // 32 keys for each wave
+constexpr int LISTED = 2048;                     // keys whose rows are looked up at a time
+
+template <bool BF16>
+__device__ __forceinline__ v4f mfma(v4i x, v4i y, v4f c) {
+    if constexpr (BF16) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8, x), __builtin_bit_cast(bf8, y), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(hf8, x), __builtin_bit_cast(hf8, y), c, 0, 0, 0);
+}
+template <bool BF16>
+__device__ __forceinline__ uint32_t bits_of(float x) {
+    if constexpr (BF16) return __builtin_bit_cast(uint16_t, (__bf16)x);
+    else return __builtin_bit_cast(uint16_t, (_Float16)x);
+}
+template <bool BF16>
+__device__ __forceinline__ float value_of(uint32_t x) {
+    if constexpr (BF16) return __uint_as_float(x << 16);
+    else return (float)__builtin_bit_cast(_Float16, (uint16_t)x);
+}
+template <bool BF16>
+__device__ __forceinline__ int pack(float lo, float hi) { return (int)(bits_of<BF16>(lo) | bits_of<BF16>(hi) << 16); }
+
+// Maximum and sum over the four lanes (l, l + 16, l + 32, l + 48) that share a query row.
+__device__ __forceinline__ float rows_max(float x) {
+    auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float rows_sum(float x) {
+    auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// The same value in all lanes, said so: it stays in scalar registers and its branches are branches.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// What a stream brings: the tokens it holds, slots of its selection (or tokens), drafted tokens, units of a (head, tile).
+struct stream {
+    int len, slots, drafted, units;
+};
+__device__ __forceinline__ stream stream_of(const attend_args& a, int b, bool tell) {
+    stream s;
+    const int most = a.cap << a.page_log2;
+    s.len = a.len[b];
+    s.drafted = a.n_new ? a.n_new[b] : a.T;
+    if (s.len < 0 || s.len > most || s.drafted < 0 || s.drafted > a.T) {
+        if (tell) atomicOr(a.flags, SWARM_DEV_BAD_LEN);
+        s.len = min(max(s.len, 0), most);
+        s.drafted = min(max(s.drafted, 0), a.T);
+    }
+    s.slots = !a.sel ? s.len : a.unit == SWARM_SEL_PAGES ? a.n_sel << a.page_log2 : a.n_sel;
+    s.units = s.drafted > 0 ? (s.slots + UNIT - 1) / UNIT : 0;
+    return s;
+}
+__device__ __forceinline__ int token_of(const attend_args& a, int row) { return a.G == 1 ? row : (int)__umulhi((uint32_t)row, a.per_g); }
+
+// Sum over the lower threads of a workgroup, and over all of them.
+__device__ __forceinline__ int block_before(int v, int* waves, int* total) {
+    int x = v;
+    const int lane = threadIdx.x % 64, w = threadIdx.x / 64;
+    for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(x, o);
+        if (lane >= o) x += y;
+    }
+    __syncthreads();
+    if (lane == 63) waves[w] = x;
+    __syncthreads();
+    int below = 0, sum = 0;
+    for (int i = 0; i < (int)blockDim.x / 64; ++i) {
+        below += i < w ? waves[i] : 0;
+        sum += waves[i];
+    }
+    *total = sum;
+    return below + x - v;
+}
+// Units of a part: part p takes units p * quota to (p + 1) * quota of the line, and unit g stands in part g / quota.
+__device__ __forceinline__ int quota_of(const attend_args& a, int units) { return max(1, (units + a.parts - 1) / a.parts); }
+
+// What a wave carries of NR * 16 query rows: lane l has row l % 16 of each 16, and of the sums of values the channels
+// 16 c + 4 (l / 16) + 0..3.  KT keys are taken at a time.
+//   TERMS: how many terms of the cache's type a weight enters its product with v as.  Two are a weight to 2^-16 and more,
+//   and cost half as many products again.
+template <bool BF16, int DP, int NR, int KT, int TERMS, bool FULL>
+struct flash {
+    static constexpr int KS = DP / 32, CT = DP / 16;
+    static constexpr int VLD = DP + 16;          // LDS row of V in elements: 32 bytes behind each, so that 16 rows' reads meet no bank twice
+    v4i qf[NR][KS], pf[NR][TERMS][KT / 32];
+    v4f o[NR][CT], sc[NR][KT / 16];
+    float m[NR], l[NR];
+
+    __device__ __forceinline__ void start(const attend_args& a, int b, int h, int row0, int drafted) {
+        const int col = threadIdx.x % 16, quad = threadIdx.x % 64 / 16;
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+            const int r = row0 + n * 16 + col, i = token_of(a, r);
+            const uint16_t* q = a.q + ((((int64_t)b * a.T + i) * a.H + h) * a.G + (r - i * a.G)) * a.d;
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                const int c = k * 4 + quad;
+                qf[n][k] = i < drafted && (FULL || c < a.d / 8) ? *reinterpret_cast<const v4i*>(q + c * 8) : v4i{0, 0, 0, 0};
+            }
+            m[n] = -INFINITY;
+            l[n] = 0.f;
+#pragma unroll
+            for (int c = 0; c < CT; ++c) o[n][c] = v4f{0.f, 0.f, 0.f, 0.f};
+        }
+    }
+    // q . k of KT keys whose rows stand in LDS.
+    template <int KLD>
+    __device__ __forceinline__ void scores(const uint16_t* ks) {
+        const int col = threadIdx.x % 16, quad = threadIdx.x % 64 / 16;
+#pragma unroll
+        for (int k = 0; k < KT / 16; ++k) {
+#pragma unroll
+            for (int n = 0; n < NR; ++n) sc[n][k] = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < KS; ++c) {
+                const v4i kf = *reinterpret_cast<const v4i*>(ks + (k * 16 + col) * KLD + c * 32 + quad * 8);
+#pragma unroll
+                for (int n = 0; n < NR; ++n) sc[n][k] = mfma<BF16>(kf, qf[n][c], sc[n][k]);
+            }
+        }
+    }
+    // V^T of 16 channels and 32 keys, as the operand of the second product: elements 0..3 and 4..7 of lane l are keys 4 (l / 16) + 0..3 and
+    // 16 more.
+    static __device__ __forceinline__ v4i get_v(const uint16_t* vs, int c) {
+        const int col = threadIdx.x % 16, quad = threadIdx.x % 64 / 16;
+        const uint16_t* from = vs + (quad * 4 + col / 4) * VLD + col % 4 * 4 + c * 16;
+        const v2i x = __builtin_bit_cast(v2i, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(from)));
+        const v2i y = __builtin_bit_cast(v2i, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(from + 16 * VLD)));
+        return v4i{x[0], x[1], y[0], y[1]};
+    }
+    // The weights of KT keys; sees[j]: which of the keys 32 j to 32 j + 31 the lane's rows see.  The maximum that weights refer to is raised only
+    // when one of the 16 rows has outgrown it by 2^8: a row's weights stay below that, which no sum here minds, and most
+    // tiles rescale nothing.
+    __device__ __forceinline__ void weigh(float scale_log2, const uint32_t* sees, bool all) {
+        const int quad = threadIdx.x % 64 / 16;
+        float mx[NR];
+        bool grown = false;
+#pragma unroll
+        for (int n = 0; n < NR; ++n)
+#pragma unroll
+            for (int e = 0; e < KT / 4; ++e) sc[n][e / 4][e % 4] *= scale_log2;
+        if (!all) {
+#pragma unroll
+            for (int e = 0; e < KT / 4; ++e) {
+                const bool seen = sees[e / 8] >> quad * 4 & 1u << (e / 4 % 2 * 16 + e % 4);
+#pragma unroll
+                for (int n = 0; n < NR; ++n) sc[n][e / 4][e % 4] = seen ? sc[n][e / 4][e % 4] : -INFINITY;
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+            mx[n] = -INFINITY;
+#pragma unroll
+            for (int e = 0; e < KT / 16; ++e) mx[n] = fmaxf(fmaxf(fmaxf(mx[n], sc[n][e][0]), fmaxf(sc[n][e][1], sc[n][e][2])), sc[n][e][3]);
+            mx[n] = rows_max(mx[n]);
+            grown |= mx[n] > m[n] + 8.f;
+        }
+        if (__any(grown)) {
+#pragma unroll
+            for (int n = 0; n < NR; ++n) {
+                const float next = fmaxf(m[n], mx[n]);
+                rescale(n, m[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[n] - next));
+                m[n] = next;
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+            const float base = m[n] == -INFINITY ? 0.f : m[n];
+#pragma unroll
+            for (int j = 0; j < KT / 32; ++j) {
+                float p[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    p[e] = __builtin_amdgcn_exp2f(sc[n][j * 2 + e / 4][e % 4] - base);
+                    l[n] += p[e];
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    pf[n][0][j][e] = pack<BF16>(p[2 * e], p[2 * e + 1]);
+                    if constexpr (TERMS == 2)
+                        pf[n][1][j][e] = pack<BF16>(p[2 * e] - value_of<BF16>((uint32_t)pf[n][0][j][e] & 0xffffu), p[2 * e + 1] - value_of<BF16>((uint32_t)pf[n][0][j][e] >> 16));
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void rescale(int n, float f) {
+        l[n] *= f;
+#pragma unroll
+        for (int c = 0; c < CT; ++c) o[n][c] *= f;
+    }
+    __device__ __forceinline__ void add(const uint16_t* vs) {
+#pragma unroll
+        for (int j = 0; j < KT / 32; ++j)
+#pragma unroll
+            for (int c = 0; c < CT; ++c) {
+                const v4i vf = get_v(vs + j * 32 * VLD, c);
+#pragma unroll
+                for (int n = 0; n < NR; ++n)
+#pragma unroll
+                    for (int k = 0; k < TERMS; ++k) o[n][c] = mfma<BF16>(vf, pf[n][k][j], o[n][c]);
+            }
+    }
+};
+
+// The same with the wave's own keys: K and V through registers into the wave's LDS, one after the other in the same place.  Whole rows
+// come from memory at a time (as the operand of the first product K would come in 64 bytes of 16 rows).
+template <bool BF16, int DP, int NR, int TERMS, bool FULL>
+struct own_keys : flash<BF16, DP, NR, 32, TERMS, FULL> {
+    typedef flash<BF16, DP, NR, 32, TERMS, FULL> base;
+    static constexpr int LPR = DP <= 64 ? 8 : DP <= 128 ? 16 : 32, RPI = 64 / LPR, VI = 32 / RPI;   // lanes on a row, rows at a time, pieces of a lane
+    static constexpr int KLD = DP + 8, VLD = base::VLD;                // LDS rows in elements: 16 rows' pieces of 16 bytes meet no bank twice
+    v4i kr[VI], vr[VI];
+    // row(key): where the row of one of the 32 keys starts, in pieces.  Pieces behind the head dimension read another one; on K's
+    // side they then count as 0.
+    template <typename ROW>
+    static __device__ __forceinline__ void load(v4i (&r)[VI], const v4i* from, int d, ROW&& row) {
+        const int lane = threadIdx.x % 64;
+        from += FULL && LPR == DP / 8 ? lane % LPR : min(lane % LPR, d / 8 - 1);
+#pragma unroll
+        for (int j = 0; j < VI; ++j) r[j] = __builtin_nontemporal_load(from + row(j * RPI + lane / LPR));
+    }
+    __device__ __forceinline__ void put_k(uint16_t* lds, int d) {
+        const int lane = threadIdx.x % 64;
+        uint16_t* to = lds + (lane / LPR) * KLD + lane % LPR * 8;
+        if (LPR == DP / 8 || lane % LPR < DP / 8) {
+#pragma unroll
+            for (int j = 0; j < VI; ++j) {
+                if (!FULL) kr[j] &= (lane % LPR - d / 8) >> 31;
+                *reinterpret_cast<v4i*>(to + j * RPI * KLD) = kr[j];
+            }
+        }
+    }
+    // Rows of keys that are not there become 0.
+    __device__ __forceinline__ void put_v(uint16_t* lds, uint32_t there) {
+        const int lane = threadIdx.x % 64;
+        if (there != ~0u) {
+            const uint32_t held = there >> (lane / LPR);
+#pragma unroll
+            for (int j = 0; j < VI; ++j)
+                if (!(held & 1u << (j * RPI))) vr[j] = v4i{0, 0, 0, 0};
+        }
+        uint16_t* to = lds + (lane / LPR) * VLD + lane % LPR * 8;
+        if (LPR == DP / 8 || lane % LPR < DP / 8) {
+#pragma unroll
+            for (int j = 0; j < VI; ++j) *reinterpret_cast<v4i*>(to + j * RPI * VLD) = vr[j];
+        }
+    }
+};
+
+// Joins what the four waves of a workgroup carry of 16 rows, through LDS (16 rows of OLD floats for each wave): calls
+// put(row, channel, sums of four channels, maximum, sum of weights) for each row and each four channels.
+template <int DP, typename F, typename PUT>
+__device__ __forceinline__ void join_waves(F& f, int n, float* os, float (*top)[16], float (*sum)[16], PUT&& put) {
+    constexpr int OLD = DP + 4;
+    const int t = threadIdx.x, col = t % 16, quad = t % 64 / 16, wave = t / 64;
+    __syncthreads();
+    const float l = rows_sum(f.l[n]);
+    if (quad == 0) top[wave][col] = f.m[n], sum[wave][col] = l;
+#pragma unroll
+    for (int c = 0; c < DP / 16; ++c) *reinterpret_cast<v4f*>(os + (wave * 16 + col) * OLD + c * 16 + quad * 4) = f.o[n][c];
+    __syncthreads();
+    for (int x = t; x < 16 * (DP / 4); x += 256) {
+        const int r = x / (DP / 4), c = x % (DP / 4) * 4;
+        const float big = fmaxf(fmaxf(top[0][r], top[1][r]), fmaxf(top[2][r], top[3][r]));
+        v4f y = {0.f, 0.f, 0.f, 0.f};
+        float z = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float g = top[w][r] == -INFINITY ? 0.f * sum[w][r] : __builtin_amdgcn_exp2f(top[w][r] - big);   // a sum that is no number stays
+            z += g * sum[w][r];
+            if (g > 0.f || g != g) y += g * *reinterpret_cast<const v4f*>(os + (w * 16 + r) * OLD + c);
+        }
+        put(r, c, y, big, z);
+    }
+}
+
+// Where a workgroup's part of the line starts and ends, and the stream and the unit within its pairs that it starts at; false if the
+// part is empty.  Workgroup 0 leaves the streams' places for the second kernel.
+__device__ __forceinline__ bool place_part(const attend_args& a, int part, int* waves, int* where, int* at, int* end, int* b, int* offset) {
+    const int t = threadIdx.x, threads = blockDim.x;
+    if (a.B <= 64) {
+        // every wave by itself
+        const int lane = t % 64, n = lane < a.B ? a.H * stream_of(a, lane, blockIdx.x == 0 && t < 64).units : 0;
+        int upto = n;
+        for (int o = 1; o < 64; o <<= 1) {
+            const int y = __shfl_up(upto, o);
+            upto += lane >= o ? y : 0;
+        }
+        const int units = __builtin_amdgcn_readlane(upto, 63), quota = quota_of(a, units);
+        if (blockIdx.x == 0) {
+            if (t < a.B) a.starts[t] = upto - n;
+            if (t == 0) a.starts[a.B] = units;
+        }
+        *at = part * quota;
+        *end = min(*at + quota, units);
+        if (*at >= *end || part >= a.parts) return false;
+        *b = __popcll(__ballot(upto <= *at));          // streams that end before it
+        *offset = *at - (__builtin_amdgcn_readlane(upto, *b) - __builtin_amdgcn_readlane(n, *b));
+        return true;
+    }
+    int quota = 0;
+    for (int pass = a.B <= threads; pass < 2; ++pass) {
+        int before = 0, all;
+        for (int base = 0; base < a.B; base += threads) {
+            const int i = base + t, n = i < a.B ? a.H * stream_of(a, i, blockIdx.x == 0).units : 0;
+            const int start = before + block_before(n, waves, &all);
+            before += all;
+            if (pass == 0 || a.B <= threads) {
+                const int units = uniform(before);
+                quota = quota_of(a, units);
+                *at = part * quota;
+                *end = min(*at + quota, units);
+            }
+            if (pass) {
+                if (start <= *at && *at < start + n) where[0] = i, where[1] = *at - start;
+                if (blockIdx.x == 0 && i < a.B) a.starts[i] = start;
+            }
+        }
+        if (blockIdx.x == 0 && t == 0) a.starts[a.B] = before;
+    }
+    __syncthreads();
+    if (*at >= *end || part >= a.parts) return false;
+    *b = uniform(where[0]);
+    *offset = uniform(where[1]);
+    return true;
+}
+
+// Looks up where the rows of keys from * UNIT .. (from + n) * UNIT of a pair start in its layer's pool, in pieces of 16 bytes, and which
+// keys are there; one that is not reads row 0 and weighs nothing.
+__device__ __forceinline__ void list_keys(const attend_args& a, const stream& s, int b, int h, int from, int n, uint32_t* listed, uint32_t* held) {
+    const int lane = threadIdx.x % 64, inside = (1 << a.page_log2) - 1;
+    __syncthreads();
+    for (int x = threadIdx.x; x < n * UNIT; x += blockDim.x) {
+        uint32_t row = 0;
+        bool there = false;
+        int pos = from * UNIT + x;
+        if (pos < s.slots) {
+            if (a.sel) {
+                const bool by_page = a.unit == SWARM_SEL_PAGES;
+                const int e = a.sel[((int64_t)b * a.H + h) * a.n_sel + (by_page ? pos >> a.page_log2 : pos)];
+                pos = by_page ? e << a.page_log2 | (pos & inside) : e;
+                if (e < 0 || e >= (by_page ? a.cap : a.cap << a.page_log2)) {
+                    if (e != -1) atomicOr(a.flags, SWARM_DEV_BAD_ENTRY);
+                    pos = s.len;
+                }
+            }
+            if (pos < s.len) {
+                const int id = a.table[(int64_t)b * a.cap + (pos >> a.page_log2)];
+                if (id < 0 || id >= a.P) atomicOr(a.flags, SWARM_DEV_BAD_PAGE);
+                else there = true, row = (((uint32_t)id * a.H + h) << a.page_log2) + (pos & inside);
+            }
+        }
+        listed[x] = row * (uint32_t)(a.d / 8);
+        const uint64_t which = __ballot(there);
+        if (lane % 32 == 0) held[x / 32] = (uint32_t)(which >> lane);
+    }
+    __syncthreads();
+}
+
+// Workgroup (part, tile of up to 32 rows): the part's keys, pair by pair, each wave 32 keys of a unit and all rows.
+template <bool BF16, int DP, int NR, bool FULL>
+__global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attend_context_kernel(attend_args a) {
+    constexpr int ROWS = 16 * NR;   // two terms of a weight: what bounds this one is memory
+    typedef own_keys<BF16, DP, NR, 2, FULL> state;
+    __shared__ __align__(16) unsigned char pool[4 * 32 * state::VLD * 2];
+    __shared__ uint32_t listed[LISTED], held[LISTED / 32];
+    __shared__ float top[4][16], sum[4][16];
+    __shared__ int waves[4], where[2];
+    static_assert(4 * 16 * (DP + 4) * 4 <= sizeof(pool), "the waves' parts of the result fit their rows of V");
+
+    const int wave = uniform(threadIdx.x / 64);
+    // workgroups of the same part and different tiles read the same keys: 8 apart, they run behind the same L2
+    const int tile = (int)(blockIdx.x / 8) % a.tiles, part = (int)(blockIdx.x / 8) / a.tiles * 8 + (int)(blockIdx.x % 8);
+    int at, end, b, offset;
+    if (!place_part(a, part, waves, where, &at, &end, &b, &offset)) return;
+    stream s = stream_of(a, b, false);
+    int h = offset / s.units, first = offset % s.units;
+    uint16_t* vs = reinterpret_cast<uint16_t*>(pool) + wave * 32 * state::VLD;
+    const uint32_t* mine = listed + wave * 32;
+    const v4i *kp = reinterpret_cast<const v4i*>(a.k), *vp = reinterpret_cast<const v4i*>(a.v);
+    state f;
+
+    for (;;) {
+        const int last = min(s.units, first + (end - at));
+        const int rows = min(s.drafted * a.G - tile * ROWS, ROWS);   // query rows here
+        if (rows > 0) {
+            f.start(a, b, h, tile * ROWS, s.drafted);
+            for (int u0 = first; u0 < last; u0 += LISTED / UNIT) {
+                const int n = min(last - u0, LISTED / UNIT);
+                list_keys(a, s, b, h, u0, n, listed, held);
+                // K and V of the next tile are on their way while one is worked on: into registers as soon as LDS has taken the last one's
+                auto row = [&](int key) { return mine[key]; };
+                f.load(f.kr, kp, a.d, row);
+                __builtin_amdgcn_sched_barrier(0);   // K's loads stay older than V's, as in the loop: whoever waits for K then need not wait for V
+                f.load(f.vr, vp, a.d, row);
+                for (int u = 0; u < n; ++u) {
+                    const uint32_t there = (uint32_t)uniform((int)held[u * 4 + wave]);
+                    const uint32_t* ahead = mine + min(u + 1, n - 1) * UNIT;
+                    auto next = [&](int key) { return ahead[key]; };
+                    f.put_k(vs, a.d);
+                    f.load(f.kr, kp, a.d, next);
+                    f.template scores<state::KLD>(vs);
+                    f.put_v(vs, there);
+                    f.load(f.vr, vp, a.d, next);
+                    f.weigh(a.scale_log2, &there, there == ~0u);
+                    f.add(vs);
+                }
+            }
+            // along the line a step goes to the next pair or to the next part: their sum names what a part found for a pair
+            const int64_t slot = (((int64_t)b * a.H + h + part) * a.tiles + tile) * ROWS;
+#pragma unroll
+            for (int r = 0; r < NR; ++r)
+                join_waves<DP>(f, r, reinterpret_cast<float*>(pool), top, sum, [&](int row, int c, v4f y, float big, float z) {
+                    if (r * 16 + row >= rows) return;
+                    *reinterpret_cast<v4f*>(a.part_o + (slot + r * 16 + row) * DP + c) = y;
+                    if (c == 0) a.part_ml[(slot + r * 16 + row) * 2] = big, a.part_ml[(slot + r * 16 + row) * 2 + 1] = z;
+                });
+        }
+        at += last - first;
+        if (at >= end) break;
+        first = 0;
+        if (++h == a.H) {
+            h = 0;
+            do s = stream_of(a, ++b, false);
+            while (s.units == 0);
+        }
+    }
+}
+
+// The same for many rows: W waves share tiles of KT keys in LDS, K and V, two of them: while one is worked on, the next comes into
+// registers, and from there into the other's place.  The matrix cores bound it, so a weight enters its product with v as one term of the cache's
+// type: off by half a step at most, as the result is by its own rounding.  (Two terms: 131000 tokens x 256 rows x 8 heads 243 us, one: 186.)
+template <bool BF16, int DP, int W, bool FULL>
+__global__ __launch_bounds__(64 * W, W <= 4 ? 2 : 1) void attend_wide_kernel(attend_args a) {
+    constexpr int NR = attend_wave_rows(DP) / 16, ROWS = 16 * NR * W, KT = DP > 128 || W == 2 ? 32 : 64, THREADS = 64 * W;
+    typedef flash<BF16, DP, NR, KT, 1, FULL> state;
+    constexpr int KLD = DP + 8, VLD = state::VLD;     // LDS rows: 16 rows' pieces of 16 bytes meet no bank twice
+    constexpr int LPR = DP / 8, PIECES = KT * LPR, MINE = (PIECES + THREADS - 1) / THREADS;
+    __shared__ __align__(16) uint16_t ks[2][KT * KLD], vs[2][KT * VLD];
+    __shared__ uint32_t listed[LISTED], held[LISTED / 32];
+    __shared__ int waves[W], where[2];
+
+    const int t = threadIdx.x, lane = t % 64, col = lane % 16, quad = lane / 16, wave = uniform(t / 64);
+    const int tile = (int)(blockIdx.x / 8) % a.tiles, part = (int)(blockIdx.x / 8) / a.tiles * 8 + (int)(blockIdx.x % 8);
+    int at, end, b, offset;
+    if (!place_part(a, part, waves, where, &at, &end, &b, &offset)) return;
+    stream s = stream_of(a, b, false);
+    int h = offset / s.units, first = offset % s.units;
+    const v4i *kp = reinterpret_cast<const v4i*>(a.k), *vp = reinterpret_cast<const v4i*>(a.v);
+    state f;
+    v4i kr[MINE], vr[MINE];
+
+    for (;;) {
+        const int last = min(s.units, first + (end - at));
+        const int rows = min(s.drafted * a.G - tile * ROWS, ROWS);   // query rows here
+        if (rows > 0) {
+            f.start(a, b, h, tile * ROWS + wave * NR * 16, s.drafted);
+            for (int u0 = first; u0 < last; u0 += LISTED / UNIT) {
+                const int n = min(last - u0, LISTED / UNIT) * (UNIT / KT);
+                list_keys(a, s, b, h, u0, n / (UNIT / KT), listed, held);
+                auto load = [&](int u) {
+#pragma unroll
+                    for (int j = 0; j < MINE; ++j) {
+                        const int x = min(t + j * THREADS, PIECES - 1), piece = x % LPR;
+                        const uint32_t row = listed[u * KT + x / LPR] + (FULL ? piece : min(piece, a.d / 8 - 1));
+                        kr[j] = kp[row];
+                        vr[j] = vp[row];
+                    }
+                };
+                // pieces behind the head dimension count as 0 on K's side; rows of keys that are not there do on V's
+                auto put = [&](int u) {
+#pragma unroll
+                    for (int j = 0; j < MINE; ++j) {
+                        const int x = t + j * THREADS, key = x / LPR, piece = x % LPR;
+                        if (PIECES % THREADS == 0 || x < PIECES) {
+                            const bool there = held[u * (KT / 32) + key / 32] >> (key % 32) & 1u;
+                            *reinterpret_cast<v4i*>(&ks[u & 1][key * KLD + piece * 8]) = FULL || piece < a.d / 8 ? kr[j] : v4i{0, 0, 0, 0};
+                            *reinterpret_cast<v4i*>(&vs[u & 1][key * VLD + piece * 8]) = there ? vr[j] : v4i{0, 0, 0, 0};
+                        }
+                    }
+                };
+                load(0);
+                put(0);
+                __syncthreads();
+                for (int u = 0; u < n; ++u) {
+                    load(min(u + 1, n - 1));
+                    uint32_t there[KT / 32], every = ~0u;
+#pragma unroll
+                    for (int j = 0; j < KT / 32; ++j) {
+                        there[j] = (uint32_t)uniform((int)held[u * (KT / 32) + j]);
+                        every &= there[j];
+                    }
+                    f.template scores<KLD>(ks[u & 1]);
+                    f.weigh(a.scale_log2, there, every == ~0u);
+                    f.add(vs[u & 1]);
+                    if (u + 1 < n) put(u + 1);
+                    __syncthreads();
+                }
+            }
+            const int64_t slot = (((int64_t)b * a.H + h + part) * a.tiles + tile) * ROWS;
+#pragma unroll
+            for (int r = 0; r < NR; ++r) {
+                const int row = (wave * NR + r) * 16 + col;
+                const float l = rows_sum(f.l[r]);
+                if (row < rows) {
+#pragma unroll
+                    for (int c = 0; c < state::CT; ++c) *reinterpret_cast<v4f*>(a.part_o + (slot + row) * DP + c * 16 + quad * 4) = f.o[r][c];
+                    if (quad == 0) a.part_ml[(slot + row) * 2] = f.m[r], a.part_ml[(slot + row) * 2 + 1] = l;
+                }
+            }
+        }
+        at += last - first;
+        if (at >= end) break;
+        first = 0;
+        if (++h == a.H) {
+            h = 0;
+            do s = stream_of(a, ++b, false);
+            while (s.units == 0);
+        }
+    }
+}
+
+// Workgroup (pair, 16 rows): the parts of the context, the drafted tokens, the end.
+template <bool BF16, int DP, bool FULL>
+__global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attend_finish_kernel(attend_args a) {
+    typedef own_keys<BF16, DP, 1, 2, FULL> state;
+    constexpr uint32_t EXP = BF16 ? 0x7f80u : 0x7c00u;
+    __shared__ __align__(16) unsigned char pool[4 * 32 * state::VLD * 2];
+    __shared__ float top[4][16], sum[4][16];
+    const int t = threadIdx.x, lane = t % 64, wave = uniform(t / 64), col = lane % 16, quad = lane / 16;
+    const int row0 = blockIdx.y * 16, h = blockIdx.x % a.H, b = blockIdx.x / a.H;
+    const int units = a.starts[a.B], start = a.starts[b];
+    const stream s = stream_of(a, b, blockIdx.y == 0 && h == 0);
+    const int rows = min(s.drafted * a.G - row0, 16);
+    if (rows <= 0) return;
+    uint16_t* vs = reinterpret_cast<uint16_t*>(pool) + wave * 32 * state::VLD;
+    const v4i *kp = reinterpret_cast<const v4i*>(a.k_new), *vp = reinterpret_cast<const v4i*>(a.v_new);
+    int j0 = a.k_new ? wave * 32 : s.drafted;         // this wave's drafted tokens: j0 and the 31 behind it, then 128 further on
+    auto row = [&](int key) { return (((uint32_t)b * a.T + min(j0 + key, s.drafted - 1)) * a.H + h) * (uint32_t)(a.d / 8); };
+    state f;
+    f.start(a, b, h, row0, s.drafted);
+    if (j0 < s.drafted) {
+        f.load(f.kr, kp, a.d, row);                   // they come while the parts are joined
+        f.load(f.vr, vp, a.d, row);
+    }
+    if (s.units > 0) {
+        const int g = start + h * s.units, quota = quota_of(a, units), p0 = g / quota, p1 = (g + s.units - 1) / quota;
+        // this row in the tiles of the first kernel
+        const int tile = row0 / a.rows, in = row0 % a.rows + min(col, rows - 1);
+        auto slot = [&](int p) { return (((int64_t)b * a.H + h + p) * a.tiles + tile) * a.rows + in; };
+        // Each wave every fourth part: the maxima first, then the sums, several parts on their way at a time.  A part without keys left zeros.
+        float big = -INFINITY;
+#pragma unroll 4
+        for (int p = p0 + wave; p <= p1; p += 4) big = fmaxf(big, a.part_ml[slot(p) * 2]);
+        f.m[0] = big;
+#pragma unroll 4
+        for (int p = p0 + wave; p <= p1; p += 4) {
+            const int64_t at = slot(p);
+            const float m = a.part_ml[at * 2], z = a.part_ml[at * 2 + 1];
+            const float* part = a.part_o + at * DP + quad * 4;
+            v4f x[state::CT];
+#pragma unroll
+            for (int c = 0; c < state::CT; ++c) x[c] = *reinterpret_cast<const v4f*>(part + c * 16);
+            const float w = m == -INFINITY ? 0.f * z : __builtin_amdgcn_exp2f(m - big);   // a sum that is no number stays
+            if (quad == 0) f.l[0] += w * z;
+#pragma unroll
+            for (int c = 0; c < state::CT; ++c) f.o[0][c] += w * x[c];
+        }
+    }
+    const int token = token_of(a, row0 + col);
+    while (j0 < s.drafted) {
+        const uint32_t there = s.drafted - j0 >= 32 ? ~0u : (1u << (s.drafted - j0)) - 1u;
+        uint32_t word = 0;
+        if (token < s.drafted) {
+            if (a.mask) word = a.mask[((int64_t)b * a.T + token) * ((a.T + 31) / 32) + j0 / 32];
+            else word = token - j0 >= 31 ? ~0u : token < j0 ? 0u : (2u << (token - j0)) - 1u;
+        }
+        // Not every row sees these: values that are not numbers stand apart.
+        bool odd = false;
+#pragma unroll
+        for (int j = 0; j < state::VI; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                uint32_t x = (uint32_t)f.vr[j][e];
+                if ((x & EXP) == EXP) x &= 0xffff0000u, odd = true;
+                if ((x & EXP << 16) == EXP << 16) x &= 0xffffu, odd = true;
+                f.vr[j][e] = (int)x;
+            }
+        f.put_k(vs, a.d);
+        f.template scores<state::KLD>(vs);
+        f.put_v(vs, there);
+        const uint32_t sees = word & there;
+        f.weigh(a.scale_log2, &sees, false);
+        f.add(vs);
+        if (__any(odd)) {
+            // One drafted token at a time: its values that are not numbers alone in LDS, and only the rows that weigh it take the product.
+#pragma unroll 1
+            for (int j = 0; j < 32; ++j) {
+                if (!(there >> j & 1u)) continue;
+                f.load(f.vr, vp, a.d, row);
+#pragma unroll
+                for (int i = 0; i < state::VI; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t y = (uint32_t)f.vr[i][e];
+                        f.vr[i][e] = (int)(((y & EXP) == EXP ? y & 0xffffu : 0u) | ((y & EXP << 16) == EXP << 16 ? y & 0xffff0000u : 0u));
+                    }
+                f.put_v(vs, 1u << j);
+                v4i alone = {0, 0, 0, 0};
+                uint32_t any = 0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (e / 4 * 16 + quad * 4 + e % 4 == j) {
+                        any = (uint32_t)f.pf[0][0][0][e / 2] & (e % 2 ? 0xffff0000u : 0xffffu);
+                        alone[e / 2] = (int)any;
+                    }
+                const bool takes = rows_max(any ? 1.f : 0.f) > 0.f;
+#pragma unroll
+                for (int c = 0; c < state::CT; ++c) {
+                    const v4f x = mfma<BF16>(f.get_v(vs, c), alone, v4f{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) f.o[0][c][r] += takes ? x[r] : 0.f;
+                }
+            }
+        }
+        j0 += UNIT;
+        if (j0 < s.drafted) {
+            f.load(f.kr, kp, a.d, row);
+            f.load(f.vr, vp, a.d, row);
+        }
+    }
+    join_waves<DP>(f, 0, reinterpret_cast<float*>(pool), top, sum, [&](int row, int c, v4f y, float m, float z) {
+        if (row >= rows) return;
+        const int i = token_of(a, row0 + row);
+        const int64_t to = (((int64_t)b * a.T + i) * a.H + h) * a.G + (row0 + row - i * a.G);
+        const bool some = z > 0.f || z != z;
+        const float g = some ? 1.f / z : 0.f;
+        if (FULL || c < a.d) *reinterpret_cast<v2i*>(a.out + to * a.d + c) = v2i{pack<BF16>(y[0] * g, y[1] * g), pack<BF16>(y[2] * g, y[3] * g)};
+        if (c == 0 && a.lse) a.lse[to] = some ? (m + log2f(z)) * 0.693147180559945309f : -INFINITY;
+    });
+}
+
+template <bool BF16, int DP, bool FULL>
+void launch_attend(const attend_args& a, hipStream_t stream) {
+    const dim3 grid((unsigned)((a.parts + 7) / 8 * 8 * a.tiles)), block(256);
+    constexpr int RW = attend_wave_rows(DP);
+    if (a.rows == 16) hipLaunchKernelGGL((attend_context_kernel<BF16, DP, 1, FULL>), grid, block, 0, stream, a);
+    else if (RW == 32 && a.rows == 32) hipLaunchKernelGGL((attend_context_kernel<BF16, DP, RW / 16, FULL>), grid, block, 0, stream, a);
+    else if (a.rows == 2 * RW) hipLaunchKernelGGL((attend_wide_kernel<BF16, DP, 2, FULL>), grid, dim3(128), 0, stream, a);
+    else if (a.rows == 4 * RW) hipLaunchKernelGGL((attend_wide_kernel<BF16, DP, 4, FULL>), grid, block, 0, stream, a);
+    else if (a.rows == 6 * RW) hipLaunchKernelGGL((attend_wide_kernel<BF16, DP, 6, FULL>), grid, dim3(384), 0, stream, a);
+    else hipLaunchKernelGGL((attend_wide_kernel<BF16, DP, 8, FULL>), grid, dim3(512), 0, stream, a);
+    hipLaunchKernelGGL((attend_finish_kernel<BF16, DP, FULL>), dim3((unsigned)(a.B * a.H), (unsigned)((a.T * a.G + 15) / 16)), block, 0, stream, a);
+}
+
+template <bool BF16, int DP>
+void launch_width(const attend_args& a, hipStream_t stream) {
+    a.d == DP ? launch_attend<BF16, DP, true>(a, stream) : launch_attend<BF16, DP, false>(a, stream);
+}
+
+template <bool BF16>
+void launch_attend_type(const attend_args& a, hipStream_t stream) {
+    const int DP = attend_width(a.d);
+    if (DP == 64) launch_width<BF16, 64>(a, stream);
+    else if (DP == 96) launch_width<BF16, 96>(a, stream);
+    else if (DP == 128) launch_width<BF16, 128>(a, stream);
+    else if (DP == 192) launch_width<BF16, 192>(a, stream);
+    else launch_width<BF16, 256>(a, stream);
+}
+
+}  // namespace

@@ -125,9 +125,12 @@ class Problem:
                         # rounding for the scale, one for the difference to the maximum in units of ln 2, 2^-22 for the exponential itself
                         e = ((d + 2) * 2.0 ** -24 * (kk.abs() @ q.abs()).max() * abs(self.scale) + 4 * 2.0 ** -24 * s[s > -math.inf].abs().max() + 2.0 ** -22).item()
                         adds = (len(s) + 64) * 2.0 ** -24
-                        # a weight stands on both sides of the division; as two terms of the cache's type it is off by 2 half steps squared at most,
-                        # or by a term below the smallest normal number (fp16: 2^-25 of the largest weight)
-                        terms = 4 * half * half + (2.0 ** -25 * len(s) if self.t is torch.float16 else 0)
+                        # What the product with v takes of a weight w, the sum of weights being that of the unrounded ones.  Up to a wave's rows (32, 16
+                        # of heads wider than 128) two terms: the second is the first one's error, rounded, so off by 2 half steps squared at most.
+                        # Above, one term: w (1 + e) with |e| <= half a step, so that sum w v is off by half a step of sum w |v| at most.
+                        # fp16 has terms below its smallest normal number, off by 2^-25; weights are below 2^8 (the maximum they refer to lags by
+                        # as much) and their sum is that of the largest one at least
+                        terms = (4 * half * half if T * G <= (16 if d > 128 else 32) else half) + (2.0 ** -25 * len(s) if self.t is torch.float16 else 0)
                         tol_o[b, i, h * G + g] = half * o.abs() * 1.01 + (2 * e + 2 * adds + terms) * (w @ vv.abs()) + torch.finfo(self.t).tiny * half
                         tol_l[b, i, h * G + g] = e + adds + 2.0 ** -22 * (1 + lse[b, i, h * G + g].abs())
         return out, lse, tol_o, tol_l
