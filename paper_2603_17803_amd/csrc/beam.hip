@@ -1,9 +1,27 @@
 // Beam search's selection over beams and vocabulary.
+//
+// One pass over the logits.  A beam's best k tokens and its normaliser ln sum exp x come from one read: a workgroup takes a slice of a
+// row in chunks of 4096 logits, holds a lower bound of the slice's k-th best logit, and puts the few that exceed it into a list in LDS, which is
+// cut down to its k best whenever it has grown.  The first bound is the k-th largest of the 256 threads' own maxima of the first chunk.  Between
+// two slices' ends a logit costs its exponential, one comparison and one addition.  What bounds it is memory for fp32 and about as much
+// the vector units for 16-bit logits (8 of them in 16 bytes, 8 exponentials at a quarter of the rate).
+//
+// A second kernel, a workgroup for each group of beams, merges the sorted lists one candidate at a time and moves the histories.
 #include <math.h>
 
+#include <type_traits>
+
 #include "common.h"
+#include "wave_ops.h"
 
 namespace {
+
+typedef int v4i __attribute__((ext_vector_type(4)));
+typedef unsigned long long u64;
+
+constexpr int CHUNK = 4096, EACH = 16;           // logits of a workgroup's step, and of a thread's
+constexpr int TRIM = 512;                        // candidates from which a list is cut down
+constexpr int MOST_LISTS = 64 * 64, STAGED = 4096;   // lists of a group; candidates of a group that its merge holds in LDS
 
 struct beam_args {
     const void* logits;
@@ -14,117 +32,346 @@ struct beam_args {
     float* out_score;
     int32_t *out_parent, *out_token, *hist_out;
     uint32_t* flags;
-    // candidates of each beam in their order: [B*K][k] scores, logits and tokens (-1: no candidate)
-    double* score;
-    float* logit;
-    int32_t* token;
-    int eos, K, V, k, hist_cap, dtype;
+    // of each slice of each beam: reference and sum of exponentials, candidates in their order (logit, token), how many
+    double* sums;                                // [rows][J]
+    float* refs;                                 // [rows][J]
+    int32_t* found;                              // [rows][J]
+    u64* lists;                                  // [rows][J][k]
+    int eos, K, V, k, hist_cap, J, per;          // per: vectors of 16 bytes of a slice
 };
 
-__device__ __forceinline__ float load_logit(const beam_args& a, int64_t at) {
+// Logits in their order as unsigned integers; 0 is below all of them.
+__device__ __forceinline__ uint32_t ordered(float x) {
+    const uint32_t u = __float_as_uint(x + 0.f);               // -0 is 0
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float logit_of(u64 key) {
+    const uint32_t u = (uint32_t)(key >> 32);
+    return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u);
+}
+// A candidate: the better logit is the larger number, and of equal ones the lower token.
+__device__ __forceinline__ u64 candidate(float x, int token) { return (u64)ordered(x) << 32 | (uint32_t)~token; }
+__device__ __forceinline__ int token_of(u64 key) { return (int)~(uint32_t)key; }
+
+template <int TYPE>
+__device__ __forceinline__ float widen(uint32_t bits) {
     float x;
-    if (a.dtype == SWARM_FP32) x = static_cast<const float*>(a.logits)[at];
-    else if (a.dtype == SWARM_BF16) x = __uint_as_float((uint32_t)static_cast<const uint16_t*>(a.logits)[at] << 16);
-    else x = (float)static_cast<const _Float16*>(a.logits)[at];
+    if (TYPE == SWARM_FP32) x = __uint_as_float(bits);
+    else if (TYPE == SWARM_BF16) x = __uint_as_float(bits << 16);
+    else x = (float)__builtin_bit_cast(_Float16, (uint16_t)bits);
     return x != x ? -INFINITY : x;
 }
 
-// Workgroup r: beam r's normaliser and its k best tokens, one round each.
-__global__ __launch_bounds__(256) void beam_row_kernel(beam_args a) {
-    __shared__ float best[256];
-    __shared__ int where[256];
-    __shared__ double sums[256];
-    const int64_t r = blockIdx.x, row = r * a.stride;
+// How many of n keys in LDS are above `key`; n is rounded up to a multiple of 2 by zeros.
+__device__ __forceinline__ int above(const u64* keys, int n, u64 key) {
+    int c = 0;
+    for (int i = 0; i < n; i += 2) {
+        const ulonglong2 x = *reinterpret_cast<const ulonglong2*>(keys + i);
+        c += x.x > key;
+        c += x.y > key;
+    }
+    return c;
+}
+
+// Cuts a list in LDS of n different keys down to its k best, in order, by a workgroup of 256; `best` has room for 256 and k more.
+// Returns how many are left.
+__device__ int trim(u64* list, int n, int k, u64* best, int* count) {
     const int t = threadIdx.x;
+    if (n > 256) {
+        // only keys from the k-th of the threads' maxima on can be among the k best
+        u64 mine = 0;
+        for (int i = t; i < n; i += 256) mine = list[i] > mine ? list[i] : mine;
+        best[t] = mine;
+        if (t == 0) *count = 0;
+        __syncthreads();
+        const int rank = above(best, 256, mine);
+        __syncthreads();
+        if (rank == k - 1) best[256] = mine;
+        __syncthreads();
+        const u64 bound = best[256];
+        // in place: what a thread reads before the barrier is written behind it
+        for (int base = 0; base < n; base += 256) {
+            const u64 x = base + t < n ? list[base + t] : 0;
+            __syncthreads();
+            if (x >= bound) list[atomicAdd(count, 1)] = x;
+        }
+        __syncthreads();
+        n = *count;
+        __syncthreads();
+    }
+    if (t == 0) list[n] = 0;
+    __syncthreads();
+    const int left = n < k ? n : k;
+    for (int i = t; i < n; i += 256) {
+        const u64 x = list[i];
+        const int rank = above(list, n, x);
+        if (rank < k) best[rank] = x;
+    }
+    __syncthreads();
+    if (t < left) list[t] = best[t];
+    if (t == 0) *count = left;
+    __syncthreads();
+    return left;
+}
+
+// Workgroup (beam, slice).
+template <int TYPE>
+__global__ __launch_bounds__(256) void beam_slice_kernel(beam_args a) {
+    constexpr int E = TYPE == SWARM_FP32 ? 4 : 8, VECS = EACH / E;      // logits of a vector, vectors of a thread's step
+    typedef typename std::conditional<TYPE == SWARM_FP32, uint32_t, uint16_t>::type word;
+    __shared__ __align__(16) u64 list[TRIM + CHUNK + 2], best[258];
+    __shared__ int count;
+    __shared__ double sum[4];
+    __shared__ float ref[4];
+    const int64_t r = blockIdx.x / a.J;
+    const int j = blockIdx.x % a.J, t = threadIdx.x, lane = t % 64;
+    const int64_t at = r * a.J + j;
     if (a.finished && a.finished[r]) {
-        for (int i = t; i < a.k; i += 256) a.token[r * a.k + i] = i == 0 ? a.eos : -1;
-        if (t == 0) a.score[r * a.k] = a.scores[r] != a.scores[r] ? -INFINITY : a.scores[r], a.logit[r * a.k] = 0.f;
+        if (t == 0) a.found[at] = j == 0 ? -1 : 0;                      // its one candidate is the second kernel's
         return;
     }
-    float after = INFINITY;
-    int last = -1;
-    double norm = 0.0;
-    for (int i = 0; i < a.k; ++i) {
-        float x = -INFINITY;
-        int at = -1;
-        for (int j = t; j < a.V; j += 256) {
-            const float y = load_logit(a, row + j);
-            const bool later = i == 0 || y < after || (y == after && j > last);
-            if (later && (at < 0 || y > x)) x = y, at = j;
-        }
-        best[t] = x;
-        where[t] = at;
-        __syncthreads();
-        for (int o = 128; o; o >>= 1) {
-            if (t < o) {
-                const float y = best[t + o];
-                const int j = where[t + o];
-                if (j >= 0 && (where[t] < 0 || y > best[t] || (y == best[t] && j < where[t]))) best[t] = y, where[t] = j;
+    const word* row = static_cast<const word*>(a.logits) + r * a.stride;
+    const int skew = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(word));      // the row's first logit in its vector
+    const word* base = row - skew;
+    const int from = j * a.per, upto = min(from + a.per, (skew + a.V + E - 1) / E);
+    auto load = [&](v4i (&v)[VECS], int chunk) {
+#pragma unroll
+        for (int i = 0; i < VECS; ++i) {
+            const int n = chunk + i * 256 + t;
+            if (n >= upto) continue;
+            const int64_t e = (int64_t)n * E;
+            if (e >= skew && e + E <= skew + a.V) {
+                v[i] = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(base + e));
+            } else {
+                // a vector that the row begins or ends in: its own logits alone
+                uint32_t w[4] = {0, 0, 0, 0};
+                for (int x = 0; x < E; ++x)
+                    if (e + x >= skew && e + x < skew + a.V) w[x * sizeof(word) / 4] |= (uint32_t)base[e + x] << (x * sizeof(word) % 4 * 8);
+                v[i] = v4i{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
             }
-            __syncthreads();
         }
-        after = best[0];
-        last = where[0];
+    };
+    auto value = [&](const v4i (&v)[VECS], int i, int e) {
+        const uint32_t w = (uint32_t)v[i][e * (int)sizeof(word) / 4];
+        return widen<TYPE>(TYPE == SWARM_FP32 ? w : e & 1 ? w >> 16 : w & 0xffffu);
+    };
+    auto token = [&](int chunk, int i, int e) { return (chunk + i * 256 + t) * E + e - skew; };
+    auto there = [&](int chunk, int i, int e) {
+        const int tok = token(chunk, i, e);
+        return chunk + i * 256 + t < upto && tok >= 0 && tok < a.V;
+    };
+
+    v4i now[VECS], next[VECS];
+    load(now, from);
+    if (from + CHUNK / E < upto) load(next, from + CHUNK / E);
+    // the first bound
+    u64 mine = 0;
+#pragma unroll
+    for (int i = 0; i < VECS; ++i)
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const u64 key = there(from, i, e) ? candidate(value(now, i, e), token(from, i, e)) : 0;
+            mine = key > mine ? key : mine;
+        }
+    best[t] = mine;
+    if (t == 0) count = 0, best[256] = 1, best[257] = 0;
+    __syncthreads();
+    const int rank = above(best, 256, mine);
+    if (mine && rank == a.k - 1) best[256] = mine;
+    if (mine && rank == 0) best[257] = mine;
+    __syncthreads();
+    u64 bound = best[256];
+    const float high = best[257] ? logit_of(best[257]) : -INFINITY;
+    // Exponentials refer to the first chunk's largest logit, in a thread that meets one far above it to that one.  Those of candidates, the largest
+    // ones, are taken in 64 bits, the others in 32, and all are added in 64: what is left of their rounding errors is far below 2^-24 of the sum.
+    float refer = high == -INFINITY ? 0.f : high;
+    double total = 0.0;
+    auto push = [&](float x, int tok) {
+        if (x > refer + 40.f) {
+            total *= exp((double)refer - x);
+            refer = x;
+        }
+        total += exp((double)x - refer);
+        list[atomicAdd(&count, 1)] = candidate(x, tok);
+    };
+#pragma unroll
+    for (int i = 0; i < VECS; ++i) {
+        float part = 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const float x = value(now, i, e);
+            if (!there(from, i, e)) continue;
+            if (candidate(x, token(from, i, e)) >= bound) push(x, token(from, i, e));
+            else part += __builtin_amdgcn_exp2f((x - refer) * 1.44269504088896341f);
+        }
+        total += part;
+    }
+    float floor = bound > 1 ? logit_of(bound) : -INFINITY;      // later logits have to be above it: equal ones lose to the lower tokens
+    for (int chunk = from + CHUNK / E; chunk < upto; chunk += CHUNK / E) {
         __syncthreads();
-        if (i == 0) {
-            double s = 0.0;
-            for (int j = t; j < a.V; j += 256) s += exp((double)load_logit(a, row + j) - after);
-            sums[t] = s;
-            __syncthreads();
-            for (int o = 128; o; o >>= 1) {
-                if (t < o) sums[t] += sums[t + o];
-                __syncthreads();
+        const int n = count;
+        __syncthreads();
+        if (n >= TRIM) {
+            trim(list, n, a.k, best, &count);
+            floor = logit_of(list[a.k - 1]);
+        }
+#pragma unroll
+        for (int i = 0; i < VECS; ++i) now[i] = next[i];
+        if (chunk + CHUNK / E < upto) load(next, chunk + CHUNK / E);
+        const bool whole = (chunk + CHUNK / E - 1 < upto - 1) && chunk * E >= skew;      // every vector of the chunk is the row's own
+#pragma unroll
+        for (int i = 0; i < VECS; ++i) {
+            float part = 0.f, top = -INFINITY, x[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                x[e] = value(now, i, e);
+                if (!whole && !there(chunk, i, e)) x[e] = -INFINITY;
+                top = fmaxf(top, x[e]);
             }
-            norm = after + log(sums[0]);
+            if (top > floor) {
+#pragma unroll 1
+                for (int e = 0; e < E; ++e) {
+                    float y = x[0];
+#pragma unroll
+                    for (int q = 1; q < E; ++q) y = q == e ? x[q] : y;
+                    if (y > floor) {
+                        push(y, token(chunk, i, e));
+#pragma unroll
+                        for (int q = 0; q < E; ++q) x[q] = q == e ? -INFINITY : x[q];
+                    }
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < E; ++e) part += __builtin_amdgcn_exp2f((x[e] - refer) * 1.44269504088896341f);
+            total += part;
         }
-        if (t == 0) {
-            const double s = a.scores[r] + ((double)after - norm);
-            a.token[r * a.k + i] = last;
-            a.logit[r * a.k + i] = after;
-            a.score[r * a.k + i] = s != s ? -INFINITY : s;
-        }
-        if (last < 0) {
-            for (int j = i + t; j < a.k; j += 256) a.token[r * a.k + j] = -1;
-            break;
-        }
+    }
+    __syncthreads();
+    const int pushed = count;
+    __syncthreads();
+    const int n = trim(list, pushed, a.k, best, &count);
+    for (int i = t; i < n; i += 256) a.lists[at * a.k + i] = list[i];
+    // the threads' sums at one reference
+    float big = refer;
+    for (int o = 32; o; o >>= 1) big = fmaxf(big, __shfl_xor(big, o));
+    if (lane == 0) ref[t / 64] = big;
+    __syncthreads();
+    big = fmaxf(fmaxf(ref[0], ref[1]), fmaxf(ref[2], ref[3]));
+    if (refer != big) total *= exp((double)refer - big);
+    for (int o = 32; o; o >>= 1) total += __shfl_xor(total, o);
+    if (lane == 0) sum[t / 64] = total;
+    __syncthreads();
+    if (t == 0) {
+        const double all = sum[0] + sum[1] + sum[2] + sum[3];
+        a.sums[at] = all;
+        a.refs[at] = all == 0.0 ? -INFINITY : big;      // a slice without a finite logit refers to nothing
+        a.found[at] = n;
     }
 }
 
-// Workgroup b: the k best of its beams' candidates, which each stand in their order, and the histories.
-__global__ __launch_bounds__(64) void beam_join_kernel(beam_args a) {
-    __shared__ int head[64];
+__device__ __forceinline__ u64 ordered(double x) {
+    const u64 u = (u64)__double_as_longlong(x + 0.0);
+    return u >> 63 ? ~u : u | (u64)1 << 63;
+}
+__device__ __forceinline__ double score_of(u64 key) { return __longlong_as_double((long long)(key >> 63 ? key & ~((u64)1 << 63) : ~key)); }
+
+// Workgroup b.  Its first wave merges: a lane has every 64th of the K * J lists and the best candidate among them, and each round takes
+// the best lane's.  Then all move the histories.
+__global__ __launch_bounds__(256) void beam_join_kernel(beam_args a) {
+    __shared__ double norm[64];                  // ln sum exp of each beam's logits; of a finished one nothing
+    __shared__ float base[64];
+    __shared__ uint8_t head[MOST_LISTS], length[MOST_LISTS];     // where each list stands, and its candidates (255: the one of a finished beam)
+    __shared__ u64 staged[STAGED];
+    __shared__ int parent[128], token[128];
     const int64_t b = blockIdx.x;
-    const int t = threadIdx.x;
-    int step = a.step ? a.step[0] : 0;
-    if (a.step && (step < 0 || step >= a.hist_cap)) {
+    const int t = threadIdx.x, lists = a.K * a.J, n_staged = lists * a.k <= STAGED ? lists * a.k : 0;
+    for (int i = t; i < lists; i += 256) head[i] = 0, length[i] = (uint8_t)a.found[b * lists + i];
+    for (int i = t; i < n_staged; i += 256) staged[i] = a.lists[b * lists * a.k + i];
+    if (t < a.K) {
+        base[t] = a.scores[b * a.K + t];
+        const int64_t at = (b * a.K + t) * a.J;
+        float big = -INFINITY;
+        double z = 0.0;
+        if (a.found[at] >= 0) {
+            for (int j = 0; j < a.J; ++j) big = fmaxf(big, a.refs[at + j]);
+            for (int j = 0; j < a.J; ++j) z += a.sums[at + j] * exp((double)a.refs[at + j] - big);
+        }
+        norm[t] = big + log(z);
+    }
+    __syncthreads();
+    if (t < 64) {
+        u64 score = 0, key = 0;                  // the lane's best candidate (0: none), its list
+        int mine = 0;
+        auto refresh = [&]() {
+            score = 0;
+            for (int i = t; i < lists; i += 64) {
+                const int beam = i / a.J, n = length[i], at = head[i];
+                if (at >= (n == 255 ? 1 : n)) continue;
+                u64 c;
+                double x = base[beam];
+                if (n == 255) {
+                    c = candidate(0.f, a.eos);
+                } else {
+                    c = n_staged ? staged[i * a.k + at] : a.lists[(b * lists + i) * a.k + at];
+                    x += (double)logit_of(c) - norm[beam];
+                }
+                const u64 s = ordered(x != x ? (double)-INFINITY : x);
+                // lists come in the order of beams, a beam's in the order of its slices
+                if (s > score || (s == score && beam == mine / a.J && c > key)) score = s, key = c, mine = i;
+            }
+        };
+        refresh();
+        for (int i = 0; i < a.k; ++i) {
+            // the largest score, then the lowest beam, the largest logit, the lowest token
+            const uint32_t hi = waveops::wave_min_u32(~(uint32_t)(score >> 32));
+            bool in = ~(uint32_t)(score >> 32) == hi;
+            const uint32_t lo = waveops::wave_min_u32(in ? ~(uint32_t)score : ~0u);
+            in = in && ~(uint32_t)score == lo;
+            const u64 top = (u64)~hi << 32 | ~lo;
+            if (top == 0) {
+                if (t == 0) parent[i] = -1, token[i] = -1, a.out_score[b * a.k + i] = -INFINITY;
+                continue;
+            }
+            u64 who = __ballot(in);
+            if (who & (who - 1)) {
+                const uint32_t beam = waveops::wave_min_u32(in ? (uint32_t)(mine / a.J) : ~0u);
+                in = in && (uint32_t)(mine / a.J) == beam;
+                const uint32_t x = waveops::wave_min_u32(in ? ~(uint32_t)(key >> 32) : ~0u);
+                in = in && ~(uint32_t)(key >> 32) == x;
+                const uint32_t y = waveops::wave_min_u32(in ? ~(uint32_t)key : ~0u);
+                in = in && ~(uint32_t)key == y;
+                who = __ballot(in);
+            }
+            if (t == __ffsll((long long)who) - 1) {
+                parent[i] = (int)(b * a.K) + mine / a.J;
+                token[i] = token_of(key);
+                a.out_score[b * a.k + i] = (float)score_of(score);
+                ++head[mine];
+                refresh();
+            }
+        }
+    }
+    __syncthreads();
+    for (int i = t; i < a.k; i += 256) a.out_parent[b * a.k + i] = parent[i], a.out_token[b * a.k + i] = token[i];
+    if (!a.hist) return;
+    int step = a.step[0];
+    const bool fits = step >= 0 && step < a.hist_cap;
+    if (!fits) {
         if (t == 0) atomicOr(a.flags, SWARM_DEV_BAD_ENTRY);
         step = step < 0 ? 0 : a.hist_cap;
     }
-    if (t < a.K) head[t] = 0;
-    __syncthreads();
-    for (int i = 0; i < a.k; ++i) {
-        int beam = -1;
-        double top = 0.0;
-        for (int j = 0; j < a.K; ++j) {
-            const int64_t at = (b * a.K + j) * a.k + head[j];
-            if (head[j] >= a.k || a.token[at] < 0) continue;
-            if (beam < 0 || a.score[at] > top) beam = j, top = a.score[at];
-        }
-        const int token = beam < 0 ? -1 : a.token[(b * a.K + beam) * a.k + head[beam]];
-        const int64_t out = b * a.k + i, parent = beam < 0 ? -1 : b * a.K + beam;
-        __syncthreads();
-        if (t == 0) {
-            a.out_score[out] = beam < 0 ? -INFINITY : (float)top;
-            a.out_parent[out] = (int)parent;
-            a.out_token[out] = token;
-            if (beam >= 0) ++head[beam];
-        }
-        if (a.hist && parent >= 0) {
-            for (int j = t; j < step; j += 64) a.hist_out[out * a.hist_cap + j] = a.hist[parent * a.hist_cap + j];
-            if (t == 0 && a.step[0] == step) a.hist_out[out * a.hist_cap + step] = token;
-        }
-        __syncthreads();
+    for (int i = t / 64; i < a.k; i += 4) {
+        if (parent[i] < 0) continue;
+        const int32_t* from = a.hist + (int64_t)parent[i] * a.hist_cap;
+        int32_t* to = a.hist_out + (b * a.k + i) * a.hist_cap;
+        for (int x = t % 64; x < step; x += 64) to[x] = from[x];
+        if (fits && t % 64 == 0) to[step] = token[i];
     }
+}
+
+template <int TYPE>
+void launch_beams(const beam_args& a, int64_t rows, hipStream_t stream) {
+    hipLaunchKernelGGL(beam_slice_kernel<TYPE>, dim3((unsigned)(rows * a.J)), dim3(256), 0, stream, a);
 }
 
 }  // namespace
@@ -151,18 +398,28 @@ extern "C" swarm_status swarm_beam_select(swarm_ctx* ctx, const void* logits, in
     const swarm_range outs[] = {{out_score, 4 * found}, {out_parent, 4 * found}, {out_token, 4 * found}, {hist_out, 4 * found * hist_cap}};
     if (swarm_overlap(outs, 4, ins, 5)) SWARM_REJECT(ctx, "beam_select: an output overlaps an input, or another output");
 
-    const swarm_status st = swarm_scratch(ctx, &ctx->beams, &ctx->beams_bytes, rows * k * 16);
+    // Slices of a row: enough workgroups for four on each compute unit, of at least one chunk each, at most 64.
+    const int each = dtype == SWARM_FP32 ? 4 : 8;
+    const int64_t vectors = ((int64_t)V + each - 1) / each + 1, most = (vectors * each + CHUNK - 1) / CHUNK;
+    int64_t J = (1024 + (int64_t)rows - 1) / (int64_t)rows;
+    J = J < most ? J : most;
+    J = J < 64 ? J : 64;
+    const size_t slices = rows * (size_t)J;
+    const swarm_status st = swarm_scratch(ctx, &ctx->beams, &ctx->beams_bytes, slices * (8 + 4 + 4 + 8 * (size_t)k));
     if (st != SWARM_OK) return st;
     beam_args a{};
     a.logits = logits, a.stride = stride, a.scores = scores, a.finished = finished;
     a.hist = hist, a.step = step, a.hist_out = hist_out;
     a.out_score = out_score, a.out_parent = out_parent, a.out_token = out_token;
     a.flags = ctx->dev_flags;
-    a.score = static_cast<double*>(ctx->beams);
-    a.logit = reinterpret_cast<float*>(a.score + rows * k);
-    a.token = reinterpret_cast<int32_t*>(a.logit + rows * k);
-    a.eos = eos, a.K = K, a.V = V, a.k = k, a.hist_cap = hist_cap, a.dtype = dtype;
-    hipLaunchKernelGGL(beam_row_kernel, dim3((unsigned)rows), dim3(256), 0, ctx->stream, a);
-    hipLaunchKernelGGL(beam_join_kernel, dim3((unsigned)B), dim3(64), 0, ctx->stream, a);
+    a.sums = static_cast<double*>(ctx->beams);
+    a.lists = reinterpret_cast<u64*>(a.sums + slices);
+    a.refs = reinterpret_cast<float*>(a.lists + slices * k);
+    a.found = reinterpret_cast<int32_t*>(a.refs + slices);
+    a.eos = eos, a.K = K, a.V = V, a.k = k, a.hist_cap = hist_cap, a.J = (int)J, a.per = (int)((vectors + J - 1) / J);
+    if (dtype == SWARM_FP32) launch_beams<SWARM_FP32>(a, (int64_t)rows, ctx->stream);
+    else if (dtype == SWARM_BF16) launch_beams<SWARM_BF16>(a, (int64_t)rows, ctx->stream);
+    else launch_beams<SWARM_FP16>(a, (int64_t)rows, ctx->stream);
+    hipLaunchKernelGGL(beam_join_kernel, dim3((unsigned)B), dim3(256), 0, ctx->stream, a);
     return swarm_check_launch(ctx, "beam_select");
 }
