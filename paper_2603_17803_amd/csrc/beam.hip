@@ -59,7 +59,7 @@ __device__ __forceinline__ float widen(uint32_t bits) {
     if (TYPE == SWARM_FP32) x = __uint_as_float(bits);
     else if (TYPE == SWARM_BF16) x = __uint_as_float(bits << 16);
     else x = (float)__builtin_bit_cast(_Float16, (uint16_t)bits);
-    return x != x ? -INFINITY : x;
+    return fmaxf(x, -INFINITY);      // the other one where x is no number
 }
 
 // How many of n keys in LDS are above `key`; n is rounded up to a multiple of 2 by zeros.
@@ -122,7 +122,7 @@ __global__ __launch_bounds__(256) void beam_slice_kernel(beam_args a) {
     __shared__ __align__(16) u64 list[TRIM + CHUNK + 2], best[258];
     __shared__ int count;
     __shared__ double sum[4];
-    __shared__ float ref[4];
+    __shared__ float ref[4], low[4];
     const int64_t r = blockIdx.x / a.J;
     const int j = blockIdx.x % a.J, t = threadIdx.x, lane = t % 64;
     const int64_t at = r * a.J + j;
@@ -182,27 +182,26 @@ __global__ __launch_bounds__(256) void beam_slice_kernel(beam_args a) {
     __syncthreads();
     u64 bound = best[256];
     const float high = best[257] ? logit_of(best[257]) : -INFINITY;
-    // Exponentials refer to the first chunk's largest logit, in a thread that meets one far above it to that one.  Those of candidates, the largest
-    // ones, are taken in 64 bits, the others in 32, and all are added in 64: what is left of their rounding errors is far below 2^-24 of the sum.
+    // Exponentials refer to the first chunk's largest logit; a thread that meets one far above it refers to that one from then on.
     float refer = high == -INFINITY ? 0.f : high;
     double total = 0.0;
     auto push = [&](float x, int tok) {
-        if (x > refer + 40.f) {
+        if (x > refer + 60.f) {
             total *= exp((double)refer - x);
             refer = x;
         }
-        total += exp((double)x - refer);
         list[atomicAdd(&count, 1)] = candidate(x, tok);
     };
+    auto weight = [&](float x, float to) { return __builtin_amdgcn_exp2f((x - to) * 1.44269504088896341f); };
 #pragma unroll
     for (int i = 0; i < VECS; ++i) {
         float part = 0.f;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const float x = value(now, i, e);
             if (!there(from, i, e)) continue;
+            const float x = value(now, i, e);
             if (candidate(x, token(from, i, e)) >= bound) push(x, token(from, i, e));
-            else part += __builtin_amdgcn_exp2f((x - refer) * 1.44269504088896341f);
+            part += weight(x, refer);
         }
         total += part;
     }
@@ -229,20 +228,12 @@ __global__ __launch_bounds__(256) void beam_slice_kernel(beam_args a) {
                 top = fmaxf(top, x[e]);
             }
             if (top > floor) {
-#pragma unroll 1
-                for (int e = 0; e < E; ++e) {
-                    float y = x[0];
 #pragma unroll
-                    for (int q = 1; q < E; ++q) y = q == e ? x[q] : y;
-                    if (y > floor) {
-                        push(y, token(chunk, i, e));
-#pragma unroll
-                        for (int q = 0; q < E; ++q) x[q] = q == e ? -INFINITY : x[q];
-                    }
-                }
+                for (int e = 0; e < E; ++e)
+                    if (x[e] > floor) push(x[e], token(chunk, i, e));
             }
 #pragma unroll
-            for (int e = 0; e < E; ++e) part += __builtin_amdgcn_exp2f((x[e] - refer) * 1.44269504088896341f);
+            for (int e = 0; e < E; ++e) part += weight(x[e], refer);
             total += part;
         }
     }
@@ -251,13 +242,19 @@ __global__ __launch_bounds__(256) void beam_slice_kernel(beam_args a) {
     __syncthreads();
     const int n = trim(list, pushed, a.k, best, &count);
     for (int i = t; i < n; i += 256) a.lists[at * a.k + i] = list[i];
-    // the threads' sums at one reference
-    float big = refer;
-    for (int o = 32; o; o >>= 1) big = fmaxf(big, __shfl_xor(big, o));
-    if (lane == 0) ref[t / 64] = big;
+    // The threads' sums at one reference.  Added in 64 bits, they are off by the rounding of the largest exponentials above all: those of the list are
+    // taken again in 64 bits in place of the 32 (unless references differ, where 1e-7 is what the logarithm is good to).
+    float big = refer, small = refer;
+    for (int o = 32; o; o >>= 1) big = fmaxf(big, __shfl_xor(big, o)), small = fminf(small, __shfl_xor(small, o));
+    if (lane == 0) ref[t / 64] = big, low[t / 64] = small;
     __syncthreads();
     big = fmaxf(fmaxf(ref[0], ref[1]), fmaxf(ref[2], ref[3]));
+    small = fminf(fminf(low[0], low[1]), fminf(low[2], low[3]));
     if (refer != big) total *= exp((double)refer - big);
+    if (small == big && t < n) {
+        const float x = logit_of(list[t]);
+        if (x > -INFINITY) total += exp((double)x - big) - weight(x, big);
+    }
     for (int o = 32; o; o >>= 1) total += __shfl_xor(total, o);
     if (lane == 0) sum[t / 64] = total;
     __syncthreads();
@@ -277,7 +274,7 @@ __device__ __forceinline__ double score_of(u64 key) { return __longlong_as_doubl
 
 // Workgroup b.  Its first wave merges: a lane has every 64th of the K * J lists and the best candidate among them, and each round takes
 // the best lane's.  Then all move the histories.
-__global__ __launch_bounds__(256) void beam_join_kernel(beam_args a) {
+__global__ __launch_bounds__(1024) void beam_join_kernel(beam_args a) {
     __shared__ double norm[64];                  // ln sum exp of each beam's logits; of a finished one nothing
     __shared__ float base[64];
     __shared__ uint8_t head[MOST_LISTS], length[MOST_LISTS];     // where each list stands, and its candidates (255: the one of a finished beam)
@@ -285,8 +282,8 @@ __global__ __launch_bounds__(256) void beam_join_kernel(beam_args a) {
     __shared__ int parent[128], token[128];
     const int64_t b = blockIdx.x;
     const int t = threadIdx.x, lists = a.K * a.J, n_staged = lists * a.k <= STAGED ? lists * a.k : 0;
-    for (int i = t; i < lists; i += 256) head[i] = 0, length[i] = (uint8_t)a.found[b * lists + i];
-    for (int i = t; i < n_staged; i += 256) staged[i] = a.lists[b * lists * a.k + i];
+    for (int i = t; i < lists; i += 1024) head[i] = 0, length[i] = (uint8_t)a.found[b * lists + i];
+    for (int i = t; i < n_staged; i += 1024) staged[i] = a.lists[b * lists * a.k + i];
     if (t < a.K) {
         base[t] = a.scores[b * a.K + t];
         const int64_t at = (b * a.K + t) * a.J;
@@ -352,7 +349,7 @@ __global__ __launch_bounds__(256) void beam_join_kernel(beam_args a) {
         }
     }
     __syncthreads();
-    for (int i = t; i < a.k; i += 256) a.out_parent[b * a.k + i] = parent[i], a.out_token[b * a.k + i] = token[i];
+    for (int i = t; i < a.k; i += 1024) a.out_parent[b * a.k + i] = parent[i], a.out_token[b * a.k + i] = token[i];
     if (!a.hist) return;
     int step = a.step[0];
     const bool fits = step >= 0 && step < a.hist_cap;
@@ -360,12 +357,36 @@ __global__ __launch_bounds__(256) void beam_join_kernel(beam_args a) {
         if (t == 0) atomicOr(a.flags, SWARM_DEV_BAD_ENTRY);
         step = step < 0 ? 0 : a.hist_cap;
     }
-    for (int i = t / 64; i < a.k; i += 4) {
+    // a wave a history, several loads on their way at a time; in 16 bytes where histories and rows allow it
+    const bool wide = ((reinterpret_cast<uintptr_t>(a.hist) | reinterpret_cast<uintptr_t>(a.hist_out)) & 15) == 0 && a.hist_cap % 4 == 0;
+    const int lane = t % 64;
+    for (int i = t / 64; i < a.k; i += 16) {
         if (parent[i] < 0) continue;
         const int32_t* from = a.hist + (int64_t)parent[i] * a.hist_cap;
         int32_t* to = a.hist_out + (b * a.k + i) * a.hist_cap;
-        for (int x = t % 64; x < step; x += 64) to[x] = from[x];
-        if (fits && t % 64 == 0) to[step] = token[i];
+        int x = 0;
+        if (wide) {
+            for (; x + 4 <= step; x += 4096) {
+                v4i v[16];
+#pragma unroll
+                for (int q = 0; q < 16; ++q)
+                    if (x + q * 256 + lane * 4 + 4 <= step) v[q] = *reinterpret_cast<const v4i*>(from + x + q * 256 + lane * 4);
+#pragma unroll
+                for (int q = 0; q < 16; ++q)
+                    if (x + q * 256 + lane * 4 + 4 <= step) *reinterpret_cast<v4i*>(to + x + q * 256 + lane * 4) = v[q];
+            }
+            x = step / 4 * 4;
+        }
+        for (; x < step; x += 1024) {
+            int v[16];
+#pragma unroll
+            for (int q = 0; q < 16; ++q)
+                if (x + q * 64 + lane < step) v[q] = from[x + q * 64 + lane];
+#pragma unroll
+            for (int q = 0; q < 16; ++q)
+                if (x + q * 64 + lane < step) to[x + q * 64 + lane] = v[q];
+        }
+        if (fits && lane == 0) to[step] = token[i];
     }
 }
 
@@ -420,6 +441,6 @@ extern "C" swarm_status swarm_beam_select(swarm_ctx* ctx, const void* logits, in
     if (dtype == SWARM_FP32) launch_beams<SWARM_FP32>(a, (int64_t)rows, ctx->stream);
     else if (dtype == SWARM_BF16) launch_beams<SWARM_BF16>(a, (int64_t)rows, ctx->stream);
     else launch_beams<SWARM_FP16>(a, (int64_t)rows, ctx->stream);
-    hipLaunchKernelGGL(beam_join_kernel, dim3((unsigned)B), dim3(256), 0, ctx->stream, a);
+    hipLaunchKernelGGL(beam_join_kernel, dim3((unsigned)B), dim3(1024), 0, ctx->stream, a);
     return swarm_check_launch(ctx, "beam_select");
 }
