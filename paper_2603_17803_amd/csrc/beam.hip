@@ -20,7 +20,7 @@ typedef int v4i __attribute__((ext_vector_type(4)));
 typedef unsigned long long u64;
 
 constexpr int CHUNK = 4096, EACH = 16;           // logits of a workgroup's step, and of a thread's
-constexpr int TRIM = 512;                        // candidates from which a list is cut down
+constexpr int TRIM = 512;                        // candidates from which a list is cut down, at most
 constexpr int MOST_LISTS = 64 * 64, STAGED = 4096;   // lists of a group; candidates of a group that its merge holds in LDS
 
 struct beam_args {
@@ -34,10 +34,10 @@ struct beam_args {
     uint32_t* flags;
     // of each slice of each beam: reference and sum of exponentials, candidates in their order (logit, token), how many
     double* sums;                                // [rows][J]
-    float* refs;                                 // [rows][J]
+    double* refs;                                // [rows][J], in units of ln 2
     int32_t* found;                              // [rows][J]
     u64* lists;                                  // [rows][J][k]
-    int eos, K, V, k, hist_cap, J, per;          // per: vectors of 16 bytes of a slice
+    int eos, K, V, k, hist_cap, J, per, trim;    // per: vectors of 16 bytes of a slice; trim: candidates from which a list is cut down
 };
 
 // Logits in their order as unsigned integers; 0 is below all of them.
@@ -53,13 +53,19 @@ __device__ __forceinline__ float logit_of(u64 key) {
 __device__ __forceinline__ u64 candidate(float x, int token) { return (u64)ordered(x) << 32 | (uint32_t)~token; }
 __device__ __forceinline__ int token_of(u64 key) { return (int)~(uint32_t)key; }
 
+// The next float below a number above -inf.
+__device__ __forceinline__ float below(float x) {
+    const uint32_t u = __float_as_uint(x + 0.f);
+    return __uint_as_float(u == 0 ? 0x80000001u : u >> 31 ? u + 1 : u - 1);
+}
+
 template <int TYPE>
 __device__ __forceinline__ float widen(uint32_t bits) {
     float x;
     if (TYPE == SWARM_FP32) x = __uint_as_float(bits);
     else if (TYPE == SWARM_BF16) x = __uint_as_float(bits << 16);
     else x = (float)__builtin_bit_cast(_Float16, (uint16_t)bits);
-    return fmaxf(x, -INFINITY);      // the other one where x is no number
+    return x;
 }
 
 // How many of n keys in LDS are above `key`; n is rounded up to a multiple of 2 by zeros.
@@ -117,7 +123,7 @@ __device__ int trim(u64* list, int n, int k, u64* best, int* count) {
 // Workgroup (beam, slice).
 template <int TYPE>
 __global__ __launch_bounds__(256) void beam_slice_kernel(beam_args a) {
-    constexpr int E = TYPE == SWARM_FP32 ? 4 : 8, VECS = EACH / E;      // logits of a vector, vectors of a thread's step
+    constexpr int E = TYPE == SWARM_FP32 ? 4 : 8, VECS = EACH / E, STEP = CHUNK / E;   // logits of a vector; vectors of a thread's step and of a chunk
     typedef typename std::conditional<TYPE == SWARM_FP32, uint32_t, uint16_t>::type word;
     __shared__ __align__(16) u64 list[TRIM + CHUNK + 2], best[258];
     __shared__ int count;
@@ -151,90 +157,97 @@ __global__ __launch_bounds__(256) void beam_slice_kernel(beam_args a) {
             }
         }
     };
-    auto value = [&](const v4i (&v)[VECS], int i, int e) {
+    auto raw = [&](const v4i (&v)[VECS], int i, int e) {
         const uint32_t w = (uint32_t)v[i][e * (int)sizeof(word) / 4];
+        if (TYPE == SWARM_BF16 && e & 1) return __uint_as_float(w & 0xffff0000u);
         return widen<TYPE>(TYPE == SWARM_FP32 ? w : e & 1 ? w >> 16 : w & 0xffffu);
     };
+    auto value = [&](const v4i (&v)[VECS], int i, int e) { return fmaxf(raw(v, i, e), -INFINITY); };   // what is no number counts as -inf
     auto token = [&](int chunk, int i, int e) { return (chunk + i * 256 + t) * E + e - skew; };
     auto there = [&](int chunk, int i, int e) {
         const int tok = token(chunk, i, e);
         return chunk + i * 256 + t < upto && tok >= 0 && tok < a.V;
     };
 
-    v4i now[VECS], next[VECS];
+    // two chunks on their way while one is worked on
+    v4i now[VECS], next[VECS], then[VECS];
     load(now, from);
-    if (from + CHUNK / E < upto) load(next, from + CHUNK / E);
-    // the first bound
-    u64 mine = 0;
+    if (from + STEP < upto) load(next, from + STEP);
+    if (from + 2 * STEP < upto) load(then, from + 2 * STEP);
+    // The first bound: the k-th largest of the maxima of 64 groups of four threads, or for many candidates of 256 threads.  At least k logits of the
+    // first chunk are not below it; 16 of 64 maxima leave hardly more of them than 16 of 256 do.
+    float mine = -INFINITY;
 #pragma unroll
     for (int i = 0; i < VECS; ++i)
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const u64 key = there(from, i, e) ? candidate(value(now, i, e), token(from, i, e)) : 0;
-            mine = key > mine ? key : mine;
-        }
-    best[t] = mine;
-    if (t == 0) count = 0, best[256] = 1, best[257] = 0;
-    __syncthreads();
-    const int rank = above(best, 256, mine);
-    if (mine && rank == a.k - 1) best[256] = mine;
-    if (mine && rank == 0) best[257] = mine;
-    __syncthreads();
-    u64 bound = best[256];
-    const float high = best[257] ? logit_of(best[257]) : -INFINITY;
-    // Exponentials refer to the first chunk's largest logit; a thread that meets one far above it refers to that one from then on.
-    float refer = high == -INFINITY ? 0.f : high;
-    double total = 0.0;
-    auto push = [&](float x, int tok) {
-        if (x > refer + 60.f) {
-            total *= exp((double)refer - x);
-            refer = x;
-        }
-        list[atomicAdd(&count, 1)] = candidate(x, tok);
-    };
-    auto weight = [&](float x, float to) { return __builtin_amdgcn_exp2f((x - to) * 1.44269504088896341f); };
-#pragma unroll
-    for (int i = 0; i < VECS; ++i) {
-        float part = 0.f;
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            if (!there(from, i, e)) continue;
-            const float x = value(now, i, e);
-            if (candidate(x, token(from, i, e)) >= bound) push(x, token(from, i, e));
-            part += weight(x, refer);
-        }
-        total += part;
+        for (int e = 0; e < E; ++e) mine = fmaxf(mine, there(from, i, e) ? raw(now, i, e) : -INFINITY);
+    const int groups = a.k <= 32 ? 64 : 256;
+    if (groups == 64) {
+        mine = fmaxf(mine, waveops::dpp_f<0xB1>(mine));        // quad_perm [1,0,3,2]
+        mine = fmaxf(mine, waveops::dpp_f<0x4E>(mine));        // quad_perm [2,3,0,1]
     }
-    float floor = bound > 1 ? logit_of(bound) : -INFINITY;      // later logits have to be above it: equal ones lose to the lower tokens
-    for (int chunk = from + CHUNK / E; chunk < upto; chunk += CHUNK / E) {
-        __syncthreads();
-        const int n = count;
-        __syncthreads();
-        if (n >= TRIM) {
-            trim(list, n, a.k, best, &count);
-            floor = logit_of(list[a.k - 1]);
-        }
-#pragma unroll
-        for (int i = 0; i < VECS; ++i) now[i] = next[i];
-        if (chunk + CHUNK / E < upto) load(next, chunk + CHUNK / E);
-        const bool whole = (chunk + CHUNK / E - 1 < upto - 1) && chunk * E >= skew;      // every vector of the chunk is the row's own
+    const int group = groups == 64 ? t / 4 : t;
+    const u64 key = candidate(mine, group);                     // of equal maxima one is the larger
+    best[group] = key;
+    if (t == 0) count = 0;
+    __syncthreads();
+    if (t < groups) {
+        const u64 own = best[t];
+        const int rank = above(best, groups, own);
+        if (rank == a.k - 1) best[256] = own;
+        if (rank == 0) best[257] = own;
+    }
+    __syncthreads();
+    const float bound = logit_of(best[256]), high = logit_of(best[257]);
+    // Logits have to be above `floor`: in the first chunk not below the bound (where that is -inf, all are taken), later above it, as equal ones lose to
+    // the lower tokens.
+    bool every = bound == -INFINITY;
+    float floor = every ? -INFINITY : below(bound);
+    // Exponentials refer to the first chunk's largest logit, as 2^(x log2 e - at); a thread that meets a logit far above it refers to that one
+    // from then on.  `at` is rounded, and stands for the logit at / log2 e exactly.
+    constexpr float LOG2E = 1.44269504088896341f;
+    float at2 = high == -INFINITY ? 0.f : high * LOG2E;
+    double total = 0.0;
+    auto weight = [&](float x, float to) { return __builtin_amdgcn_exp2f(__builtin_fmaf(x, LOG2E, -to)); };
+    for (int chunk = from; chunk < upto; chunk += STEP) {
+        const bool whole = chunk > from && chunk + STEP < upto;      // neither the first nor the last: every vector is the row's own
 #pragma unroll
         for (int i = 0; i < VECS; ++i) {
             float part = 0.f, top = -INFINITY, x[E];
+            if (whole) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                x[e] = value(now, i, e);
-                if (!whole && !there(chunk, i, e)) x[e] = -INFINITY;
-                top = fmaxf(top, x[e]);
+                for (int e = 0; e < E; ++e) x[e] = raw(now, i, e);
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e) x[e] = there(chunk, i, e) ? raw(now, i, e) : -INFINITY;
             }
-            if (top > floor) {
+#pragma unroll
+            for (int e = 0; e < E; e += 2) top = fmaxf(fmaxf(top, x[e]), x[e + 1]);
+            if (top > floor || every) {
+                if (top * LOG2E > at2 + 80.f) {
+                    total *= exp2((double)at2 - (double)(top * LOG2E));
+                    at2 = top * LOG2E;
+                }
 #pragma unroll
                 for (int e = 0; e < E; ++e)
-                    if (x[e] > floor) push(x[e], token(chunk, i, e));
+                    if (x[e] > floor || (every && there(chunk, i, e))) list[atomicAdd(&count, 1)] = candidate(fmaxf(x[e], -INFINITY), token(chunk, i, e));
             }
 #pragma unroll
-            for (int e = 0; e < E; ++e) part += weight(x[e], refer);
+            for (int e = 0; e < E; ++e) part += weight(x[e], at2);
             total += part;
+            now[i] = next[i], next[i] = then[i];
+        }
+        if (chunk + 3 * STEP < upto) load(then, chunk + 3 * STEP);
+        every = false;
+        floor = fmaxf(floor, bound);
+        if (chunk + STEP < upto) {
+            __syncthreads();
+            const int n = count;
+            __syncthreads();
+            if (n >= a.trim) {
+                trim(list, n, a.k, best, &count);
+                floor = logit_of(list[a.k - 1]);
+            }
         }
     }
     __syncthreads();
@@ -242,18 +255,38 @@ __global__ __launch_bounds__(256) void beam_slice_kernel(beam_args a) {
     __syncthreads();
     const int n = trim(list, pushed, a.k, best, &count);
     for (int i = t; i < n; i += 256) a.lists[at * a.k + i] = list[i];
-    // The threads' sums at one reference.  Added in 64 bits, they are off by the rounding of the largest exponentials above all: those of the list are
-    // taken again in 64 bits in place of the 32 (unless references differ, where 1e-7 is what the logarithm is good to).
-    float big = refer, small = refer;
-    for (int o = 32; o; o >>= 1) big = fmaxf(big, __shfl_xor(big, o)), small = fminf(small, __shfl_xor(small, o));
-    if (lane == 0) ref[t / 64] = big, low[t / 64] = small;
-    __syncthreads();
-    big = fmaxf(fmaxf(ref[0], ref[1]), fmaxf(ref[2], ref[3]));
-    small = fminf(fminf(low[0], low[1]), fminf(low[2], low[3]));
-    if (refer != big) total *= exp((double)refer - big);
-    if (small == big && t < n) {
-        const float x = logit_of(list[t]);
-        if (x > -INFINITY) total += exp((double)x - big) - weight(x, big);
+    double big;
+    if (__syncthreads_or(total != total || !(fabsf(at2) < 1e5f))) {
+        // A logit that is no number or infinite, or logits so large that 2^(x log2 e - at) says nothing: the sum again, in 64 bits, referred to the
+        // best candidate.  (A candidate of +inf leaves no number, as the definition does.)
+        const double best_logit = n ? logit_of(list[0]) : -INFINITY;
+        total = 0.0;
+        for (int chunk = from; chunk < upto; chunk += STEP) {
+            load(now, chunk);
+#pragma unroll
+            for (int i = 0; i < VECS; ++i)
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const float x = there(chunk, i, e) ? value(now, i, e) : -INFINITY;
+                    if (x > -INFINITY) total += exp((double)x - best_logit);
+                }
+        }
+        big = best_logit * 1.4426950408889634074;
+    } else {
+        // The threads' sums at one reference.  Added in 64 bits, they are off by the rounding of the largest exponentials above all: those of the list
+        // are taken again in 64 bits in place of the 32 (unless references differ, where 1e-7 is what the logarithm is good to).
+        float high2 = at2, small = at2;
+        for (int o = 32; o; o >>= 1) high2 = fmaxf(high2, __shfl_xor(high2, o)), small = fminf(small, __shfl_xor(small, o));
+        if (lane == 0) ref[t / 64] = high2, low[t / 64] = small;
+        __syncthreads();
+        high2 = fmaxf(fmaxf(ref[0], ref[1]), fmaxf(ref[2], ref[3]));
+        small = fminf(fminf(low[0], low[1]), fminf(low[2], low[3]));
+        if (at2 != high2) total *= exp2((double)at2 - (double)high2);
+        if (small == high2 && t < n) {
+            const float x = logit_of(list[t]);
+            if (x > -INFINITY) total += exp2((double)x * 1.4426950408889634074 - (double)high2) - weight(x, high2);
+        }
+        big = high2;
     }
     for (int o = 32; o; o >>= 1) total += __shfl_xor(total, o);
     if (lane == 0) sum[t / 64] = total;
@@ -261,7 +294,7 @@ __global__ __launch_bounds__(256) void beam_slice_kernel(beam_args a) {
     if (t == 0) {
         const double all = sum[0] + sum[1] + sum[2] + sum[3];
         a.sums[at] = all;
-        a.refs[at] = all == 0.0 ? -INFINITY : big;      // a slice without a finite logit refers to nothing
+        a.refs[at] = all == 0.0 ? (double)-INFINITY : big;      // a slice without a finite logit refers to nothing
         a.found[at] = n;
     }
 }
@@ -277,32 +310,31 @@ __device__ __forceinline__ double score_of(u64 key) { return __longlong_as_doubl
 __global__ __launch_bounds__(1024) void beam_join_kernel(beam_args a) {
     __shared__ double norm[64];                  // ln sum exp of each beam's logits; of a finished one nothing
     __shared__ float base[64];
-    __shared__ uint8_t head[MOST_LISTS], length[MOST_LISTS];     // where each list stands, and its candidates (255: the one of a finished beam)
+    __shared__ uint8_t head[MOST_LISTS], length[MOST_LISTS], beams[MOST_LISTS];   // where each list stands, its candidates (255: the one of a finished beam), its beam
     __shared__ u64 staged[STAGED];
     __shared__ int parent[128], token[128];
     const int64_t b = blockIdx.x;
     const int t = threadIdx.x, lists = a.K * a.J, n_staged = lists * a.k <= STAGED ? lists * a.k : 0;
-    for (int i = t; i < lists; i += 1024) head[i] = 0, length[i] = (uint8_t)a.found[b * lists + i];
+    for (int i = t; i < lists; i += 1024) head[i] = 0, length[i] = (uint8_t)a.found[b * lists + i], beams[i] = (uint8_t)(i / a.J);
     for (int i = t; i < n_staged; i += 1024) staged[i] = a.lists[b * lists * a.k + i];
     if (t < a.K) {
         base[t] = a.scores[b * a.K + t];
         const int64_t at = (b * a.K + t) * a.J;
-        float big = -INFINITY;
-        double z = 0.0;
+        double big = -INFINITY, z = 0.0;
         if (a.found[at] >= 0) {
-            for (int j = 0; j < a.J; ++j) big = fmaxf(big, a.refs[at + j]);
-            for (int j = 0; j < a.J; ++j) z += a.sums[at + j] * exp((double)a.refs[at + j] - big);
+            for (int j = 0; j < a.J; ++j) big = fmax(big, a.refs[at + j]);
+            for (int j = 0; j < a.J; ++j) z += a.sums[at + j] * exp2(a.refs[at + j] - big);
         }
-        norm[t] = big + log(z);
+        norm[t] = big * 0.69314718055994530942 + log(z);
     }
     __syncthreads();
     if (t < 64) {
         u64 score = 0, key = 0;                  // the lane's best candidate (0: none), its list
-        int mine = 0;
+        int mine = 0, owner = 0;                 // and that one's beam
         auto refresh = [&]() {
             score = 0;
             for (int i = t; i < lists; i += 64) {
-                const int beam = i / a.J, n = length[i], at = head[i];
+                const int beam = beams[i], n = length[i], at = head[i];
                 if (at >= (n == 255 ? 1 : n)) continue;
                 u64 c;
                 double x = base[beam];
@@ -314,7 +346,7 @@ __global__ __launch_bounds__(1024) void beam_join_kernel(beam_args a) {
                 }
                 const u64 s = ordered(x != x ? (double)-INFINITY : x);
                 // lists come in the order of beams, a beam's in the order of its slices
-                if (s > score || (s == score && beam == mine / a.J && c > key)) score = s, key = c, mine = i;
+                if (s > score || (s == score && beam == owner && c > key)) score = s, key = c, mine = i, owner = beam;
             }
         };
         refresh();
@@ -331,8 +363,8 @@ __global__ __launch_bounds__(1024) void beam_join_kernel(beam_args a) {
             }
             u64 who = __ballot(in);
             if (who & (who - 1)) {
-                const uint32_t beam = waveops::wave_min_u32(in ? (uint32_t)(mine / a.J) : ~0u);
-                in = in && (uint32_t)(mine / a.J) == beam;
+                const uint32_t beam = waveops::wave_min_u32(in ? (uint32_t)owner : ~0u);
+                in = in && (uint32_t)owner == beam;
                 const uint32_t x = waveops::wave_min_u32(in ? ~(uint32_t)(key >> 32) : ~0u);
                 in = in && ~(uint32_t)(key >> 32) == x;
                 const uint32_t y = waveops::wave_min_u32(in ? ~(uint32_t)key : ~0u);
@@ -340,7 +372,7 @@ __global__ __launch_bounds__(1024) void beam_join_kernel(beam_args a) {
                 who = __ballot(in);
             }
             if (t == __ffsll((long long)who) - 1) {
-                parent[i] = (int)(b * a.K) + mine / a.J;
+                parent[i] = (int)(b * a.K) + owner;
                 token[i] = token_of(key);
                 a.out_score[b * a.k + i] = (float)score_of(score);
                 ++head[mine];
@@ -426,7 +458,7 @@ extern "C" swarm_status swarm_beam_select(swarm_ctx* ctx, const void* logits, in
     J = J < most ? J : most;
     J = J < 64 ? J : 64;
     const size_t slices = rows * (size_t)J;
-    const swarm_status st = swarm_scratch(ctx, &ctx->beams, &ctx->beams_bytes, slices * (8 + 4 + 4 + 8 * (size_t)k));
+    const swarm_status st = swarm_scratch(ctx, &ctx->beams, &ctx->beams_bytes, slices * (8 + 8 + 4 + 8 * (size_t)k));
     if (st != SWARM_OK) return st;
     beam_args a{};
     a.logits = logits, a.stride = stride, a.scores = scores, a.finished = finished;
@@ -435,9 +467,10 @@ extern "C" swarm_status swarm_beam_select(swarm_ctx* ctx, const void* logits, in
     a.flags = ctx->dev_flags;
     a.sums = static_cast<double*>(ctx->beams);
     a.lists = reinterpret_cast<u64*>(a.sums + slices);
-    a.refs = reinterpret_cast<float*>(a.lists + slices * k);
+    a.refs = reinterpret_cast<double*>(a.lists + slices * k);
     a.found = reinterpret_cast<int32_t*>(a.refs + slices);
     a.eos = eos, a.K = K, a.V = V, a.k = k, a.hist_cap = hist_cap, a.J = (int)J, a.per = (int)((vectors + J - 1) / J);
+    a.trim = 4 * k < 48 ? 48 : 4 * k;            // 512 at most
     if (dtype == SWARM_FP32) launch_beams<SWARM_FP32>(a, (int64_t)rows, ctx->stream);
     else if (dtype == SWARM_BF16) launch_beams<SWARM_BF16>(a, (int64_t)rows, ctx->stream);
     else launch_beams<SWARM_FP16>(a, (int64_t)rows, ctx->stream);
