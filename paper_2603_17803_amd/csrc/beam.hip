@@ -140,21 +140,32 @@ __global__ __launch_bounds__(256) void beam_slice_kernel(beam_args a) {
     const int skew = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(word));      // the row's first logit in its vector
     const word* base = row - skew;
     const int from = j * a.per, upto = min(from + a.per, (skew + a.V + E - 1) / E);
+    // whether all vectors of a chunk are the slice's, and whole in the row
+    auto whole = [&](int chunk) { return chunk + STEP <= upto && chunk * (int64_t)E >= skew && (chunk + STEP) * (int64_t)E <= skew + (int64_t)a.V; };
     auto load = [&](v4i (&v)[VECS], int chunk) {
+        if (chunk >= upto) return;
+        if (whole(chunk)) {
+            const v4i* p = reinterpret_cast<const v4i*>(base) + chunk + t;
+#pragma unroll
+            for (int i = 0; i < VECS; ++i) v[i] = __builtin_nontemporal_load(p + i * 256);
+            return;
+        }
+        // the row's own logits alone of the vectors that it begins and ends in
 #pragma unroll
         for (int i = 0; i < VECS; ++i) {
-            const int n = chunk + i * 256 + t;
-            if (n >= upto) continue;
-            const int64_t e = (int64_t)n * E;
-            if (e >= skew && e + E <= skew + a.V) {
-                v[i] = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(base + e));
-            } else {
-                // a vector that the row begins or ends in: its own logits alone
-                uint32_t w[4] = {0, 0, 0, 0};
-                for (int x = 0; x < E; ++x)
-                    if (e + x >= skew && e + x < skew + a.V) w[x * sizeof(word) / 4] |= (uint32_t)base[e + x] << (x * sizeof(word) % 4 * 8);
-                v[i] = v4i{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
+            const int64_t e = (int64_t)(chunk + i * 256 + t) * E;
+            uint32_t w[4] = {0, 0, 0, 0};
+            if (chunk + i * 256 + t < upto) {
+                if (e >= skew && e + E <= skew + a.V) {
+                    const v4i x = *reinterpret_cast<const v4i*>(base + e);
+                    for (int q = 0; q < 4; ++q) w[q] = (uint32_t)x[q];
+                } else {
+#pragma unroll
+                    for (int x = 0; x < E; ++x)
+                        if (e + x >= skew && e + x < skew + a.V) w[x * sizeof(word) / 4] |= (uint32_t)base[e + x] << (x * sizeof(word) % 4 * 8);
+                }
             }
+            v[i] = v4i{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
         }
     };
     auto raw = [&](const v4i (&v)[VECS], int i, int e) {
@@ -162,25 +173,22 @@ __global__ __launch_bounds__(256) void beam_slice_kernel(beam_args a) {
         if (TYPE == SWARM_BF16 && e & 1) return __uint_as_float(w & 0xffff0000u);
         return widen<TYPE>(TYPE == SWARM_FP32 ? w : e & 1 ? w >> 16 : w & 0xffffu);
     };
-    auto value = [&](const v4i (&v)[VECS], int i, int e) { return fmaxf(raw(v, i, e), -INFINITY); };   // what is no number counts as -inf
     auto token = [&](int chunk, int i, int e) { return (chunk + i * 256 + t) * E + e - skew; };
     auto there = [&](int chunk, int i, int e) {
         const int tok = token(chunk, i, e);
         return chunk + i * 256 + t < upto && tok >= 0 && tok < a.V;
     };
 
-    // two chunks on their way while one is worked on
-    v4i now[VECS], next[VECS], then[VECS];
-    load(now, from);
-    if (from + STEP < upto) load(next, from + STEP);
-    if (from + 2 * STEP < upto) load(then, from + 2 * STEP);
+    v4i even[VECS], odd[VECS];                   // the chunks of even and odd number: one on its way while the other is worked on
+    load(even, from);
+    load(odd, from + STEP);
     // The first bound: the k-th largest of the maxima of 64 groups of four threads, or for many candidates of 256 threads.  At least k logits of the
     // first chunk are not below it; 16 of 64 maxima leave hardly more of them than 16 of 256 do.
     float mine = -INFINITY;
 #pragma unroll
     for (int i = 0; i < VECS; ++i)
 #pragma unroll
-        for (int e = 0; e < E; ++e) mine = fmaxf(mine, there(from, i, e) ? raw(now, i, e) : -INFINITY);
+        for (int e = 0; e < E; ++e) mine = fmaxf(mine, there(from, i, e) ? raw(even, i, e) : -INFINITY);
     const int groups = a.k <= 32 ? 64 : 256;
     if (groups == 64) {
         mine = fmaxf(mine, waveops::dpp_f<0xB1>(mine));        // quad_perm [1,0,3,2]
@@ -209,17 +217,27 @@ __global__ __launch_bounds__(256) void beam_slice_kernel(beam_args a) {
     float at2 = high == -INFINITY ? 0.f : high * LOG2E;
     double total = 0.0;
     auto weight = [&](float x, float to) { return __builtin_amdgcn_exp2f(__builtin_fmaf(x, LOG2E, -to)); };
-    for (int chunk = from; chunk < upto; chunk += STEP) {
-        const bool whole = chunk > from && chunk + STEP < upto;      // neither the first nor the last: every vector is the row's own
+    auto take = [&](const v4i (&v)[VECS], int chunk) {
+        if (chunk > from) {
+            __syncthreads();
+            const int n = count;
+            __syncthreads();
+            every = false;
+            floor = fmaxf(floor, bound);
+            if (n >= a.trim) {
+                trim(list, n, a.k, best, &count);
+                floor = logit_of(list[a.k - 1]);
+            }
+        }
+        const bool plain = whole(chunk);
 #pragma unroll
         for (int i = 0; i < VECS; ++i) {
             float part = 0.f, top = -INFINITY, x[E];
-            if (whole) {
 #pragma unroll
-                for (int e = 0; e < E; ++e) x[e] = raw(now, i, e);
-            } else {
+            for (int e = 0; e < E; ++e) x[e] = raw(v, i, e);
+            if (!plain) {
 #pragma unroll
-                for (int e = 0; e < E; ++e) x[e] = there(chunk, i, e) ? raw(now, i, e) : -INFINITY;
+                for (int e = 0; e < E; ++e) x[e] = there(chunk, i, e) ? x[e] : -INFINITY;
             }
 #pragma unroll
             for (int e = 0; e < E; e += 2) top = fmaxf(fmaxf(top, x[e]), x[e + 1]);
@@ -228,27 +246,29 @@ __global__ __launch_bounds__(256) void beam_slice_kernel(beam_args a) {
                     total *= exp2((double)at2 - (double)(top * LOG2E));
                     at2 = top * LOG2E;
                 }
+                uint32_t m = 0;
 #pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (x[e] > floor || (every && there(chunk, i, e))) list[atomicAdd(&count, 1)] = candidate(fmaxf(x[e], -INFINITY), token(chunk, i, e));
+                for (int e = 0; e < E; ++e) m |= x[e] > floor || (every && there(chunk, i, e)) ? 1u << e : 0u;
+                while (m) {
+                    const int e = __ffs((int)m) - 1;
+                    m &= m - 1;
+                    float y = x[0];
+#pragma unroll
+                    for (int q = 1; q < E; ++q) y = e == q ? x[q] : y;
+                    list[atomicAdd(&count, 1)] = candidate(fmaxf(y, -INFINITY), token(chunk, i, e));
+                }
             }
 #pragma unroll
             for (int e = 0; e < E; ++e) part += weight(x[e], at2);
             total += part;
-            now[i] = next[i], next[i] = then[i];
         }
-        if (chunk + 3 * STEP < upto) load(then, chunk + 3 * STEP);
-        every = false;
-        floor = fmaxf(floor, bound);
-        if (chunk + STEP < upto) {
-            __syncthreads();
-            const int n = count;
-            __syncthreads();
-            if (n >= a.trim) {
-                trim(list, n, a.k, best, &count);
-                floor = logit_of(list[a.k - 1]);
-            }
-        }
+    };
+    for (int chunk = from; chunk < upto; chunk += 2 * STEP) {
+        take(even, chunk);
+        load(even, chunk + 2 * STEP);
+        if (chunk + STEP >= upto) break;
+        take(odd, chunk + STEP);
+        load(odd, chunk + 3 * STEP);
     }
     __syncthreads();
     const int pushed = count;
@@ -262,12 +282,12 @@ __global__ __launch_bounds__(256) void beam_slice_kernel(beam_args a) {
         const double best_logit = n ? logit_of(list[0]) : -INFINITY;
         total = 0.0;
         for (int chunk = from; chunk < upto; chunk += STEP) {
-            load(now, chunk);
+            load(even, chunk);
 #pragma unroll
             for (int i = 0; i < VECS; ++i)
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    const float x = there(chunk, i, e) ? value(now, i, e) : -INFINITY;
+                    const float x = there(chunk, i, e) ? fmaxf(raw(even, i, e), -INFINITY) : -INFINITY;
                     if (x > -INFINITY) total += exp((double)x - best_logit);
                 }
         }
