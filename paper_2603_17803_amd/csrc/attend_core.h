@@ -574,13 +574,15 @@ __global__ __launch_bounds__(64 * W, W <= 4 ? 2 : 1) void attend_wide_kernel(att
     }
 }
 
-// Workgroup (pair, 16 rows): the parts of the context, the drafted tokens, the end.
-template <bool BF16, int DP, bool FULL>
-__global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attend_finish_kernel(attend_args a) {
+// Workgroup (pair, 16 rows): the parts of the context, the drafted tokens, the end.  W waves share the parts and the drafted tokens: one
+// where a pair has few parts, as many rows fill the device then, or four where it has many.  (24 x 4 pairs of 168 rows, 3 parts
+// each: 21 us with four waves, 10 with one; 8 pairs of 4 rows, 33 parts each: 10 and 25.)
+template <bool BF16, int DP, int W, bool FULL>
+__global__ __launch_bounds__(64 * W, DP > 128 ? 1 : 2) void attend_finish_kernel(attend_args a) {
     typedef own_keys<BF16, DP, 1, 2, FULL> state;
     constexpr uint32_t EXP = BF16 ? 0x7f80u : 0x7c00u;
-    __shared__ __align__(16) unsigned char pool[4 * 32 * state::VLD * 2];
-    __shared__ float top[4][16], sum[4][16];
+    __shared__ __align__(16) unsigned char pool[W * 32 * state::VLD * 2];
+    __shared__ float top[W][16], sum[W][16];
     const int t = threadIdx.x, lane = t % 64, wave = uniform(t / 64), col = lane % 16, quad = lane / 16;
     const int row0 = blockIdx.y * 16, h = blockIdx.x % a.H, b = blockIdx.x / a.H;
     const int units = a.starts[a.B], start = a.starts[b];
@@ -589,7 +591,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attend_finish_kernel(at
     if (rows <= 0) return;
     uint16_t* vs = reinterpret_cast<uint16_t*>(pool) + wave * 32 * state::VLD;
     const v4i *kp = reinterpret_cast<const v4i*>(a.k_new), *vp = reinterpret_cast<const v4i*>(a.v_new);
-    int j0 = a.k_new ? wave * 32 : s.drafted;         // this wave's drafted tokens: j0 and the 31 behind it, then 128 further on
+    int j0 = a.k_new ? wave * 32 : s.drafted;         // this wave's drafted tokens: j0 and the 31 behind it, then 32 W further on
     auto row = [&](int key) { return (((uint32_t)b * a.T + min(j0 + key, s.drafted - 1)) * a.H + h) * (uint32_t)(a.d / 8); };
     state f;
     f.start(a, b, h, row0, s.drafted);
@@ -602,13 +604,13 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attend_finish_kernel(at
         // this row in the tiles of the first kernel
         const int tile = row0 / a.rows, in = row0 % a.rows + min(col, rows - 1);
         auto slot = [&](int p) { return (((int64_t)b * a.H + h + p) * a.tiles + tile) * a.rows + in; };
-        // Each wave every fourth part: the maxima first, then the sums, several parts on their way at a time.  A part without keys left zeros.
+        // Each wave every W-th part: the maxima first, then the sums, several parts on their way at a time.  A part without keys left zeros.
         float big = -INFINITY;
 #pragma unroll 4
-        for (int p = p0 + wave; p <= p1; p += 4) big = fmaxf(big, a.part_ml[slot(p) * 2]);
+        for (int p = p0 + wave; p <= p1; p += W) big = fmaxf(big, a.part_ml[slot(p) * 2]);
         f.m[0] = big;
 #pragma unroll 4
-        for (int p = p0 + wave; p <= p1; p += 4) {
+        for (int p = p0 + wave; p <= p1; p += W) {
             const int64_t at = slot(p);
             const float m = a.part_ml[at * 2], z = a.part_ml[at * 2 + 1];
             const float* part = a.part_o + at * DP + quad * 4;
@@ -630,23 +632,29 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attend_finish_kernel(at
             else word = token - j0 >= 31 ? ~0u : token < j0 ? 0u : (2u << (token - j0)) - 1u;
         }
         // Not every row sees these: values that are not numbers stand apart.
-        bool odd = false;
+        typedef uint16_t v2h __attribute__((ext_vector_type(2)));
+        v2h largest = {0, 0};
 #pragma unroll
         for (int j = 0; j < state::VI; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                uint32_t x = (uint32_t)f.vr[j][e];
-                if ((x & EXP) == EXP) x &= 0xffff0000u, odd = true;
-                if ((x & EXP << 16) == EXP << 16) x &= 0xffffu, odd = true;
-                f.vr[j][e] = (int)x;
-            }
+            for (int e = 0; e < 4; ++e) largest = __builtin_elementwise_max(largest, __builtin_bit_cast(v2h, f.vr[j][e] & 0x7fff7fff));
+        const bool odd = __any(largest[0] >= EXP || largest[1] >= EXP);
+        if (odd) {
+#pragma unroll
+            for (int j = 0; j < state::VI; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t x = (uint32_t)f.vr[j][e];
+                    f.vr[j][e] = (int)(x & ((x & EXP) == EXP ? 0xffff0000u : ~0u) & ((x & EXP << 16) == EXP << 16 ? 0xffffu : ~0u));
+                }
+        }
         f.put_k(vs, a.d);
         f.template scores<state::KLD>(vs);
         f.put_v(vs, there);
         const uint32_t sees = word & there;
         f.weigh(a.scale_log2, &sees, false);
         f.add(vs);
-        if (__any(odd)) {
+        if (odd) {
             // One drafted token at a time: its values that are not numbers alone in LDS, and only the rows that weigh it take the product.
 #pragma unroll 1
             for (int j = 0; j < 32; ++j) {
@@ -677,13 +685,13 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attend_finish_kernel(at
                 }
             }
         }
-        j0 += UNIT;
+        j0 += 32 * W;
         if (j0 < s.drafted) {
             f.load(f.kr, kp, a.d, row);
             f.load(f.vr, vp, a.d, row);
         }
     }
-    join_waves<DP>(f, 0, reinterpret_cast<float*>(pool), top, sum, [&](int row, int c, v4f y, float m, float z) {
+    auto put = [&](int row, int c, v4f y, float m, float z) {
         if (row >= rows) return;
         const int i = token_of(a, row0 + row);
         const int64_t to = (((int64_t)b * a.T + i) * a.H + h) * a.G + (row0 + row - i * a.G);
@@ -691,7 +699,14 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attend_finish_kernel(at
         const float g = some ? 1.f / z : 0.f;
         if (FULL || c < a.d) *reinterpret_cast<v2i*>(a.out + to * a.d + c) = v2i{pack<BF16>(y[0] * g, y[1] * g), pack<BF16>(y[2] * g, y[3] * g)};
         if (c == 0 && a.lse) a.lse[to] = some ? (m + log2f(z)) * 0.693147180559945309f : -INFINITY;
-    });
+    };
+    if constexpr (W == 1) {
+        const float z = rows_sum(f.l[0]);
+#pragma unroll
+        for (int c = 0; c < state::CT; ++c) put(col, c * 16 + quad * 4, f.o[0][c], f.m[0], z);
+    } else {
+        join_waves<DP>(f, 0, reinterpret_cast<float*>(pool), top, sum, put);
+    }
 }
 
 template <bool BF16, int DP, bool FULL>
@@ -704,7 +719,9 @@ void launch_attend(const attend_args& a, hipStream_t stream) {
     else if (a.rows == 4 * RW) hipLaunchKernelGGL((attend_wide_kernel<BF16, DP, 4, FULL>), grid, block, 0, stream, a);
     else if (a.rows == 6 * RW) hipLaunchKernelGGL((attend_wide_kernel<BF16, DP, 6, FULL>), grid, dim3(384), 0, stream, a);
     else hipLaunchKernelGGL((attend_wide_kernel<BF16, DP, 8, FULL>), grid, dim3(512), 0, stream, a);
-    hipLaunchKernelGGL((attend_finish_kernel<BF16, DP, FULL>), dim3((unsigned)(a.B * a.H), (unsigned)((a.T * a.G + 15) / 16)), block, 0, stream, a);
+    const dim3 rows((unsigned)(a.B * a.H), (unsigned)((a.T * a.G + 15) / 16));
+    if (a.parts <= 4 * a.B * a.H && a.T <= 64) hipLaunchKernelGGL((attend_finish_kernel<BF16, DP, 1, FULL>), rows, dim3(64), 0, stream, a);
+    else hipLaunchKernelGGL((attend_finish_kernel<BF16, DP, 4, FULL>), rows, block, 0, stream, a);
 }
 
 template <bool BF16, int DP>
