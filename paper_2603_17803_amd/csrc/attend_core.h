@@ -303,7 +303,7 @@ struct own_keys : flash<BF16, DP, NR, 32, TERMS, FULL> {
 
 // Joins what the four waves of a workgroup carry of 16 rows, through LDS (16 rows of OLD floats for each wave): calls
 // put(row, channel, sums of four channels, maximum, sum of weights) for each row and each four channels.
-template <int DP, typename F, typename PUT>
+template <int DP, int W, typename F, typename PUT>
 __device__ __forceinline__ void join_waves(F& f, int n, float* os, float (*top)[16], float (*sum)[16], PUT&& put) {
     constexpr int OLD = DP + 4;
     const int t = threadIdx.x, col = t % 16, quad = t % 64 / 16, wave = t / 64;
@@ -313,13 +313,15 @@ __device__ __forceinline__ void join_waves(F& f, int n, float* os, float (*top)[
 #pragma unroll
     for (int c = 0; c < DP / 16; ++c) *reinterpret_cast<v4f*>(os + (wave * 16 + col) * OLD + c * 16 + quad * 4) = f.o[n][c];
     __syncthreads();
-    for (int x = t; x < 16 * (DP / 4); x += 256) {
+    for (int x = t; x < 16 * (DP / 4); x += 64 * W) {
         const int r = x / (DP / 4), c = x % (DP / 4) * 4;
-        const float big = fmaxf(fmaxf(top[0][r], top[1][r]), fmaxf(top[2][r], top[3][r]));
+        float big = top[0][r];
+#pragma unroll
+        for (int w = 1; w < W; ++w) big = fmaxf(big, top[w][r]);
         v4f y = {0.f, 0.f, 0.f, 0.f};
         float z = 0.f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
+        for (int w = 0; w < W; ++w) {
             const float g = top[w][r] == -INFINITY ? 0.f * sum[w][r] : __builtin_amdgcn_exp2f(top[w][r] - big);   // a sum that is no number stays
             z += g * sum[w][r];
             if (g > 0.f || g != g) y += g * *reinterpret_cast<const v4f*>(os + (w * 16 + r) * OLD + c);
@@ -464,7 +466,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attend_context_kernel(a
             const int64_t slot = (((int64_t)b * a.H + h + part) * a.tiles + tile) * ROWS;
 #pragma unroll
             for (int r = 0; r < NR; ++r)
-                join_waves<DP>(f, r, reinterpret_cast<float*>(pool), top, sum, [&](int row, int c, v4f y, float big, float z) {
+                join_waves<DP, 4>(f, r, reinterpret_cast<float*>(pool), top, sum, [&](int row, int c, v4f y, float big, float z) {
                     if (r * 16 + row >= rows) return;
                     *reinterpret_cast<v4f*>(a.part_o + (slot + r * 16 + row) * DP + c) = y;
                     if (c == 0) a.part_ml[(slot + r * 16 + row) * 2] = big, a.part_ml[(slot + r * 16 + row) * 2 + 1] = z;
@@ -705,7 +707,7 @@ __global__ __launch_bounds__(64 * W, DP > 128 ? 1 : 2) void attend_finish_kernel
 #pragma unroll
         for (int c = 0; c < state::CT; ++c) put(col, c * 16 + quad * 4, f.o[0][c], f.m[0], z);
     } else {
-        join_waves<DP>(f, 0, reinterpret_cast<float*>(pool), top, sum, put);
+        join_waves<DP, W>(f, 0, reinterpret_cast<float*>(pool), top, sum, put);
     }
 }
 
@@ -721,7 +723,7 @@ void launch_attend(const attend_args& a, hipStream_t stream) {
     else hipLaunchKernelGGL((attend_wide_kernel<BF16, DP, 8, FULL>), grid, dim3(512), 0, stream, a);
     const dim3 rows((unsigned)(a.B * a.H), (unsigned)((a.T * a.G + 15) / 16));
     if (a.parts <= 4 * a.B * a.H && a.T <= 64) hipLaunchKernelGGL((attend_finish_kernel<BF16, DP, 1, FULL>), rows, dim3(64), 0, stream, a);
-    else hipLaunchKernelGGL((attend_finish_kernel<BF16, DP, 4, FULL>), rows, block, 0, stream, a);
+    else hipLaunchKernelGGL((attend_finish_kernel<BF16, DP, 8, FULL>), rows, dim3(512), 0, stream, a);
 }
 
 template <bool BF16, int DP>
