@@ -349,39 +349,46 @@ __global__ __launch_bounds__(1024) void beam_join_kernel(beam_args a) {
     }
     __syncthreads();
     if (t < 64) {
-        u64 score = 0, key = 0;                  // the lane's best candidate (0: none), its list
-        int mine = 0, owner = 0;                 // and that one's beam
+        // The lane's best candidate (score 0: none), its beam and its list; where it has one list alone, the candidate behind it too.
+        u64 score = 0, key = 0, behind = 0;
+        int owner = 0, mine = t, at = 0, n = 0;
+        const bool single = lists <= 64;
+        auto key_of = [&](int list, int place) { return n_staged ? staged[list * a.k + place] : a.lists[(b * lists + list) * a.k + place]; };
+        auto score_of_key = [&](int beam, u64 c, bool finished) {
+            double x = base[beam];
+            if (!finished) x += (double)logit_of(c) - norm[beam];
+            return ordered(x != x ? (double)-INFINITY : x);
+        };
         auto refresh = [&]() {
             score = 0;
             for (int i = t; i < lists; i += 64) {
-                const int beam = beams[i], n = length[i], at = head[i];
-                if (at >= (n == 255 ? 1 : n)) continue;
-                u64 c;
-                double x = base[beam];
-                if (n == 255) {
-                    c = candidate(0.f, a.eos);
-                } else {
-                    c = n_staged ? staged[i * a.k + at] : a.lists[(b * lists + i) * a.k + at];
-                    x += (double)logit_of(c) - norm[beam];
-                }
-                const u64 s = ordered(x != x ? (double)-INFINITY : x);
+                const int beam = beams[i], count = length[i], place = head[i];
+                const bool finished = count == 255;
+                if (place >= (finished ? 1 : count)) continue;
+                const u64 c = finished ? candidate(0.f, a.eos) : key_of(i, place), s = score_of_key(beam, c, finished);
                 // lists come in the order of beams, a beam's in the order of its slices
                 if (s > score || (s == score && beam == owner && c > key)) score = s, key = c, mine = i, owner = beam;
             }
         };
         refresh();
+        if (single && t < lists) {
+            n = length[t] == 255 ? 1 : length[t];
+            if (n > 1) behind = key_of(t, 1);
+        }
         for (int i = 0; i < a.k; ++i) {
             // the largest score, then the lowest beam, the largest logit, the lowest token
             const uint32_t hi = waveops::wave_min_u32(~(uint32_t)(score >> 32));
             bool in = ~(uint32_t)(score >> 32) == hi;
-            const uint32_t lo = waveops::wave_min_u32(in ? ~(uint32_t)score : ~0u);
-            in = in && ~(uint32_t)score == lo;
-            const u64 top = (u64)~hi << 32 | ~lo;
-            if (top == 0) {
+            u64 who = __ballot(in);
+            if (who & (who - 1)) {
+                const uint32_t lo = waveops::wave_min_u32(in ? ~(uint32_t)score : ~0u);
+                in = in && ~(uint32_t)score == lo;
+                who = __ballot(in);
+            }
+            if (hi == ~0u) {
                 if (t == 0) parent[i] = -1, token[i] = -1, a.out_score[b * a.k + i] = -INFINITY;
                 continue;
             }
-            u64 who = __ballot(in);
             if (who & (who - 1)) {
                 const uint32_t beam = waveops::wave_min_u32(in ? (uint32_t)owner : ~0u);
                 in = in && (uint32_t)owner == beam;
@@ -395,8 +402,15 @@ __global__ __launch_bounds__(1024) void beam_join_kernel(beam_args a) {
                 parent[i] = (int)(b * a.K) + owner;
                 token[i] = token_of(key);
                 a.out_score[b * a.k + i] = (float)score_of(score);
-                ++head[mine];
-                refresh();
+                if (single) {
+                    ++at;
+                    key = behind;
+                    score = at < n ? score_of_key(owner, key, false) : 0;
+                    if (at + 1 < n) behind = key_of(t, at + 1);
+                } else {
+                    ++head[mine];
+                    refresh();
+                }
             }
         }
     }
