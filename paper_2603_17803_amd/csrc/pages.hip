@@ -28,7 +28,8 @@ struct fork_args {
     v4i *k, *v;                                  // the pool in pieces of 16 bytes
     const int32_t *table, *len, *refs, *parent, *room;
     int32_t *table_out, *len_out, *refs_out;
-    int32_t *fresh, *start, *free_ids, *state;   // new pages of each row, where they start in free_ids; state[0]: how many are free
+    int32_t *fresh, *start, *lens, *free_ids, *state;   // new pages of each row, where they start in free_ids, its length; state[0]: how many are free
+    int32_t* copies;                             // [rows][3]: page that a row copies from and to (-1: none), tokens of it
     uint32_t* flags;
     int L, P, H, page, chunks, rows, cap;        // chunks of 16 bytes in a token of one head
 };
@@ -110,7 +111,7 @@ __global__ __launch_bounds__(256) void fork_plan_kernel(fork_args a) {
         if (t == 0 && a.room && (int64_t)len + max(a.room[r], 0) > (int64_t)a.cap * a.page) atomicOr(a.flags, SWARM_DEV_NO_PAGE);
     }
     for (int j = t; j < a.cap; j += 256) out[j] = j < kept ? a.table[(int64_t)p * a.cap + j] : -1;
-    if (t == 0) a.fresh[r] = need - kept, a.len_out[r] = len;
+    if (t == 0) a.fresh[r] = need - kept, a.lens[r] = len;
 }
 
 // One workgroup: where each row's new pages start, and the lowest free ids for all of them.
@@ -140,44 +141,163 @@ __global__ __launch_bounds__(1024) void fork_scan_kernel(fork_args a) {
     if (t == 0) a.state[0] = min(found, want);
 }
 
-// Workgroups (r, y): row r's new pages, and the copy of a partly filled one, the layers divided over y.
+// Workgroup r: row r's new pages, where there are any, its length and what it copies.
 __global__ __launch_bounds__(256) void fork_fill_kernel(fork_args a) {
     const int r = blockIdx.x, t = threadIdx.x, p = parent_of(a, r);
-    const int n = a.fresh[r], start = a.start[r], have = a.state[0];
-    if (p < 0 || n == 0) return;
-    const int32_t* old = a.table + (int64_t)p * a.cap;
+    const int n = a.fresh[r], start = a.start[r], have = a.state[0], len = a.lens[r];
+    const int kept = p < 0 ? 0 : pages_needed(a, len, r) - n, full = len / a.page, tail = len % a.page;
     int32_t* out = a.table_out + (int64_t)r * a.cap;
-    // this row's first new slot: the slots before it were written by the plan
-    const int len = a.len_out[r], need = pages_needed(a, len, r), kept = need - n, full = len / a.page, tail = len % a.page;
-    const bool copies = tail > 0 && kept <= full;
-    if (blockIdx.y == 0) {
-        for (int j = t; j < n; j += 256) {
-            if (start + j < have) {
-                const int id = a.free_ids[start + j];
-                out[kept + j] = id;
-                a.refs_out[id] = 1;
-            } else {
-                atomicOr(a.flags, SWARM_DEV_NO_PAGE);
-            }
+    for (int j = t; j < n; j += 256) {
+        if (start + j < have) {
+            const int id = a.free_ids[start + j];
+            out[kept + j] = id;
+            a.refs_out[id] = 1;
+        } else {
+            atomicOr(a.flags, SWARM_DEV_NO_PAGE);
         }
     }
-    if (!copies || start >= have) return;
-    const int src = old[full], dst = a.free_ids[start];
-    const int piece = tail * a.chunks;
+    if (t == 0) {
+        const bool copies = p >= 0 && tail > 0 && kept <= full, there = n > 0 && start < have;
+        a.len_out[r] = copies && !there ? full * a.page : len;
+        a.copies[3 * r] = copies && there ? a.table[(int64_t)p * a.cap + full] : -1;
+        a.copies[3 * r + 1] = copies && there ? a.free_ids[start] : -1;
+        a.copies[3 * r + 2] = tail;
+    }
+}
+
+// The same in one workgroup, for tables of up to 4096 slots (16 waves' rows in pieces of 64, four a wave) and pools that LDS holds: what bounds a small
+// fork is launches and the trips to memory between them.  A wave has every 16th row, and holds its rows' slots in registers.  (4 rows of 64 slots:
+// 7 us here, 20 by the four kernels; 256 rows of 128 slots, with more turns a wave: 100 here, 22 there.)
+constexpr int ONE_ROWS = 1024, ONE_SLOTS = 4, ONE_PAGES = 8192;
+__global__ __launch_bounds__(1024) void fork_one_kernel(fork_args a) {
+    __shared__ int refs[ONE_PAGES], ids[ONE_PAGES];
+    __shared__ int held[ONE_ROWS], kids[ONE_ROWS], eldest[ONE_ROWS], lens[ONE_ROWS], rooms[ONE_ROWS], parents[ONE_ROWS];
+    __shared__ int old_kept[ONE_ROWS], old_full[ONE_ROWS], new_kept[ONE_ROWS], new_need[ONE_ROWS], start[ONE_ROWS], waves[16];
+    const int t = threadIdx.x, lane = t % 64, wave = __builtin_amdgcn_readfirstlane(t / 64), pieces = (a.cap + 63) / 64;
+    int slot[ONE_SLOTS];
+    {
+        int r = wave, c = 0;
+#pragma unroll
+        for (int q = 0; q < ONE_SLOTS; ++q) {
+            slot[q] = r < a.rows && c * 64 + lane < a.cap ? a.table[(int64_t)r * a.cap + c * 64 + lane] : -1;
+            if (++c == pieces) c = 0, r += 16;
+        }
+    }
+    const int mine = t < a.rows ? parent_of(a, t) : -1, room = t < a.rows && a.room ? max(a.room[t], 0) : 0, had = t < a.rows ? a.len[t] : 0;
+    if (t < a.rows && a.parent[t] != mine) atomicOr(a.flags, SWARM_DEV_BAD_ENTRY);
+    for (int i = t; i < a.P; i += 1024) refs[i] = a.refs[i];
+    held[t] = a.cap;
+    parents[t] = mine;
+    rooms[t] = room;
+    kids[t] = 0;
+    eldest[t] = a.rows;
+    __syncthreads();
+    if (mine >= 0) atomicAdd(&kids[mine], 1), atomicMin(&eldest[mine], t);
+    {
+        int r = wave, c = 0;
+#pragma unroll
+        for (int q = 0; q < ONE_SLOTS; ++q) {
+            if (r < a.rows && c * 64 + lane < a.cap && (slot[q] < 0 || slot[q] >= a.P)) {
+                if (slot[q] != -1) atomicOr(a.flags, SWARM_DEV_BAD_PAGE);
+                atomicMin(&held[r], c * 64 + lane);
+            }
+            if (++c == pieces) c = 0, r += 16;
+        }
+    }
+    __syncthreads();
+    auto need_of = [&](int len, int more) {
+        const int64_t n = ((int64_t)len + more + a.page - 1) / a.page;
+        return n > a.cap ? a.cap : (int)n;
+    };
+    if (t < a.rows) {
+        const int64_t most = (int64_t)held[t] * a.page;
+        if (had < 0 || had > most) atomicOr(a.flags, SWARM_DEV_BAD_LEN);
+        lens[t] = had < 0 ? 0 : had > most ? (int)most : had;
+    }
+    __syncthreads();
+    // as a new row: pages that it needs and keeps; as an old one: full ones, which all its children share, and those that the eldest keeps
+    const int len = mine >= 0 ? lens[mine] : 0, need = mine >= 0 ? need_of(len, room) : 0;
+    const int kept = mine < 0 ? 0 : eldest[mine] == t ? min(held[mine], need) : len / a.page;
+    if (mine >= 0 && (int64_t)len + room > (int64_t)a.cap * a.page) atomicOr(a.flags, SWARM_DEV_NO_PAGE);
+    new_kept[t] = kept;
+    new_need[t] = need;
+    if (t < a.rows) {
+        old_full[t] = lens[t] / a.page;
+        old_kept[t] = kids[t] ? min(held[t], need_of(lens[t], rooms[eldest[t]])) : 0;
+    }
+    int want;
+    const int before = block_excl_scan(t < a.rows ? need - kept : 0, waves, &want);
+    start[t] = before;
+    __syncthreads();
+    {
+        int r = wave, c = 0;
+#pragma unroll
+        for (int q = 0; q < ONE_SLOTS; ++q) {
+            const int j = c * 64 + lane;
+            if (r < a.rows && j < a.cap && slot[q] >= 0 && slot[q] < a.P) {
+                const int now = j < old_full[r] ? kids[r] : j < old_kept[r] ? 1 : 0;
+                if (now != 1) atomicAdd(&refs[slot[q]], now - 1);
+            }
+            // in its place what the new row takes over
+            const int p = r < a.rows ? parents[r] : -1;
+            slot[q] = p >= 0 && j < new_kept[r] ? a.table[(int64_t)p * a.cap + j] : -1;
+            if (++c == pieces) c = 0, r += 16;
+        }
+    }
+    const int tail_page = mine >= 0 && len / a.page < a.cap ? a.table[(int64_t)mine * a.cap + len / a.page] : -1;
+    __syncthreads();
+    int found = 0;
+    for (int at = 0; at < a.P && found < want; at += 1024) {
+        int n;
+        const bool is_free = at + t < a.P && refs[at + t] == 0;
+        const int place = found + block_excl_scan(is_free, waves, &n);
+        if (is_free && place < want) ids[place] = at + t;
+        found += n;
+    }
+    const int have = min(found, want);
+    __syncthreads();
+    {
+        int r = wave, c = 0;
+#pragma unroll
+        for (int q = 0; q < ONE_SLOTS; ++q) {
+            const int j = c * 64 + lane;
+            if (r < a.rows && j < a.cap) {
+                const int keep = new_kept[r];
+                if (j >= keep && j < new_need[r]) {
+                    if (start[r] + j - keep < have) {
+                        slot[q] = ids[start[r] + j - keep];
+                        refs[slot[q]] = 1;
+                    } else {
+                        atomicOr(a.flags, SWARM_DEV_NO_PAGE);
+                    }
+                }
+                a.table_out[(int64_t)r * a.cap + j] = slot[q];
+            }
+            if (++c == pieces) c = 0, r += 16;
+        }
+    }
+    if (t < a.rows) {
+        const int full = len / a.page, tail = len % a.page;
+        const bool copies = mine >= 0 && tail > 0 && kept <= full, there = need > kept && start[t] < have;
+        a.len_out[t] = copies && !there ? full * a.page : len;
+        a.copies[3 * t] = copies && there ? tail_page : -1;
+        a.copies[3 * t + 1] = copies && there ? ids[start[t]] : -1;
+        a.copies[3 * t + 2] = tail;
+    }
+    __syncthreads();
+    for (int i = t; i < a.P; i += 1024) a.refs_out[i] = refs[i];
+}
+
+// Workgroups (r, y): the tokens that row r copies, layers and heads divided over y.
+__global__ __launch_bounds__(256) void fork_copy_kernel(fork_args a) {
+    const int r = blockIdx.x, src = a.copies[3 * r], dst = a.copies[3 * r + 1], piece = a.copies[3 * r + 2] * a.chunks;
+    if (src < 0) return;
     for (int part = blockIdx.y; part < a.L * a.H * 2; part += gridDim.y) {
         v4i* pool = part & 1 ? a.v : a.k;
         const int64_t l = part / 2 / a.H, h = part / 2 % a.H;
         const int64_t from = ((l * a.P + src) * a.H + h) * a.page * a.chunks, to = ((l * a.P + dst) * a.H + h) * a.page * a.chunks;
-        for (int i = t; i < piece; i += 256) pool[to + i] = pool[from + i];
+        for (int i = threadIdx.x; i < piece; i += 256) pool[to + i] = pool[from + i];
     }
-}
-
-// Rows whose partly filled page found no place end at their last full page.
-__global__ void fork_cut_kernel(fork_args a) {
-    const int r = blockIdx.x * blockDim.x + threadIdx.x;
-    if (r >= a.rows || parent_of(a, r) < 0) return;
-    const int len = a.len_out[r], full = len / a.page;
-    if (len % a.page && (full >= a.cap || a.table_out[(int64_t)r * a.cap + full] < 0)) a.len_out[r] = full * a.page;
 }
 
 // ---- append -------------------------------------------------------------------------------------------------------------
@@ -378,25 +498,33 @@ swarm_status swarm_cache_fork(swarm_ctx* ctx, const swarm_cache* c, const int32_
     const swarm_range outs[] = {{table_out, ins[2].bytes}, {len_out, ins[3].bytes}, {refs_out, ins[4].bytes}};
     if (swarm_overlap(outs, 3, ins, 7)) SWARM_REJECT(ctx, "cache_fork: an output overlaps an input, or another output");
 
-    // new pages of each row, their starts, the ids for all of them (no more than there are pages), one count
-    st = swarm_scratch(ctx, &ctx->pages, &ctx->pages_bytes, 4 * (2 * (size_t)c->rows + c->P + 4));
+    // new pages of each row, their starts, lengths and copies, the ids for all new pages (no more than there are pages), one count
+    st = swarm_scratch(ctx, &ctx->pages, &ctx->pages_bytes, 4 * (6 * (size_t)c->rows + c->P + 4));
     if (st != SWARM_OK) return st;
     fork_args a{};
     a.k = static_cast<v4i*>(c->k);
     a.v = static_cast<v4i*>(c->v);
     a.table = c->table, a.len = c->len, a.refs = c->refs, a.parent = parent, a.room = room;
     a.table_out = table_out, a.len_out = len_out, a.refs_out = refs_out;
-    a.fresh = static_cast<int32_t*>(ctx->pages);
+    a.state = static_cast<int32_t*>(ctx->pages);
+    a.fresh = a.state + 4;
     a.start = a.fresh + c->rows;
-    a.state = a.start + c->rows;
-    a.free_ids = a.state + 4;
+    a.lens = a.start + c->rows;
+    a.copies = a.lens + c->rows;
+    a.free_ids = a.copies + 3 * (size_t)c->rows;
     a.flags = ctx->dev_flags;
     a.L = c->L, a.P = c->P, a.H = c->H, a.page = c->page, a.chunks = c->d / 8, a.rows = c->rows, a.cap = c->cap;
-    hipLaunchKernelGGL(copy_words_kernel, dim3((unsigned)((c->P + 255) / 256 < 1024 ? (c->P + 255) / 256 : 1024)), dim3(256), 0, ctx->stream, c->refs, refs_out, c->P);
-    hipLaunchKernelGGL(fork_plan_kernel, dim3((unsigned)c->rows), dim3(256), 0, ctx->stream, a);
-    hipLaunchKernelGGL(fork_scan_kernel, dim3(1), dim3(1024), 0, ctx->stream, a);
-    hipLaunchKernelGGL(fork_fill_kernel, dim3((unsigned)c->rows, 64), dim3(256), 0, ctx->stream, a);
-    hipLaunchKernelGGL(fork_cut_kernel, dim3((unsigned)((c->rows + 255) / 256)), dim3(256), 0, ctx->stream, a);
+    const int turns = (c->rows + 15) / 16 * ((c->cap + 63) / 64);       // slots of a lane where one workgroup has all rows
+    if (c->rows <= ONE_ROWS && c->P <= ONE_PAGES && turns <= ONE_SLOTS) {
+        hipLaunchKernelGGL(fork_one_kernel, dim3(1), dim3(1024), 0, ctx->stream, a);
+    } else {
+        hipLaunchKernelGGL(copy_words_kernel, dim3((unsigned)((c->P + 255) / 256 < 1024 ? (c->P + 255) / 256 : 1024)), dim3(256), 0, ctx->stream, c->refs, refs_out, c->P);
+        hipLaunchKernelGGL(fork_plan_kernel, dim3((unsigned)c->rows), dim3(256), 0, ctx->stream, a);
+        hipLaunchKernelGGL(fork_scan_kernel, dim3(1), dim3(1024), 0, ctx->stream, a);
+        hipLaunchKernelGGL(fork_fill_kernel, dim3((unsigned)c->rows), dim3(256), 0, ctx->stream, a);
+    }
+    const int parts = 2 * c->L * c->H;
+    hipLaunchKernelGGL(fork_copy_kernel, dim3((unsigned)c->rows, (unsigned)(parts < 64 ? parts : 64)), dim3(256), 0, ctx->stream, a);
     return swarm_check_launch(ctx, "cache_fork");
 }
 
