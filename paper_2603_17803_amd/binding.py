@@ -8,9 +8,8 @@ there is no CPU fallback.
 from __future__ import annotations
 
 import ctypes as C
-import dataclasses
 import os
-from typing import Any, Optional, Tuple
+from typing import Any, NamedTuple, Optional, Tuple
 
 from . import build as _build
 
@@ -44,8 +43,7 @@ class swarm_cache(C.Structure):
                 ("rows", C.c_int32), ("cap", C.c_int32)]
 
 
-@dataclasses.dataclass(frozen=True)
-class Cache:
+class Cache(NamedTuple):
     """The tensors of a paged cache (swarm_cache): k, v [L][P][H][page][d] bf16 or fp16; table int32 [rows][cap], length int32 [rows],
     refs int32 [P].  The calls that change it write the pool in place and return a Cache with new tables."""
     k: Any
@@ -305,6 +303,9 @@ class Swarm:
             raise RuntimeError("paper_2603_17803_amd needs an MI355X; no GPU is visible")
         self.device = torch.device("cuda", device)
         self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
+        self._index = device
+        self._i32, self._f32 = torch.int32, torch.float32
+        self._kinds = {torch.bfloat16: SWARM_BF16, torch.float16: SWARM_FP16, torch.float32: SWARM_FP32}
         self.ctx = swarm_create(device, self.stream.cuda_stream)
 
     def close(self):
@@ -603,35 +604,32 @@ class Swarm:
         self._check("swarm_step", rc)
         return out_idx, out_scores, out
 
-    def _cache(self, cache: Cache, refs: bool) -> swarm_cache:
-        """The C form of a cache after the checks of its tensors' shapes; `refs`: the call reads the counts."""
-        torch = self.torch
-        k = cache.k
-        if k.dim() != 5 or tuple(cache.v.shape) != tuple(k.shape) or cache.v.dtype is not k.dtype:
-            raise ValueError("k and v must be [L][P][H][page][d] of one type")
-        L, P, H, page, d = k.shape
-        if cache.table.dim() != 2 or cache.length.shape != (cache.table.shape[0],):
-            raise ValueError("table must be [rows][cap] and length [rows]")
-        if (refs or cache.refs is not None) and (cache.refs is None or cache.refs.shape != (P,)):
-            raise ValueError("refs must be [P]")
-        dtype = self._dtype(k, "k", (torch.bfloat16, torch.float16))
-        return swarm_cache(dtype, self._dev(k, None, "k"), self._dev(cache.v, None, "v"), L, P, H, page, d, self._dev(cache.table, torch.int32, "table"),
-                           self._dev(cache.length, torch.int32, "length"), None if cache.refs is None else self._dev(cache.refs, torch.int32, "refs"),
-                           cache.table.shape[0], cache.table.shape[1])
+    # Small calls take about as long on the host as on the device: the checks of the calls around the cache go tensor by tensor without
+    # anything made on the way, and the outputs that a call makes itself are not checked.
 
-    def _dtype(self, t, name: str, allowed) -> int:
-        torch = self.torch
-        if t.dtype not in allowed:
-            raise ValueError(f"{name} has dtype {t.dtype}, expected one of {allowed}")
-        return {torch.bfloat16: SWARM_BF16, torch.float16: SWARM_FP16, torch.float32: SWARM_FP32}[t.dtype]
-
-    def _opt(self, t, shape, dtype, name: str):
-        """Address of an optional tensor of a given shape; None stays None."""
+    def _at(self, t, shape, dtype, name: str):
+        """Address of a tensor of a given shape and type on the context's device; None stays None."""
         if t is None:
             return None
-        if t.shape != shape:
-            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-        return self._dev(t, dtype, name)
+        if t.shape != shape or t.dtype is not dtype or t.get_device() != self._index or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {self.device}, not {t.dtype} {tuple(t.shape)} on {t.device}")
+        return t.data_ptr()
+
+    def _cache(self, cache: Cache, refs: bool) -> swarm_cache:
+        """The C form of a cache after the checks of its tensors; `refs`: the call reads the counts."""
+        k, v, table, length, counts = cache
+        shape, dtype = k.shape, k.dtype
+        if len(shape) != 5 or dtype not in self._kinds or dtype is self._f32:
+            raise ValueError("k and v must be [L][P][H][page][d], bf16 or fp16")
+        L, P, H, page, d = shape
+        i32 = self._i32
+        if table.dim() != 2:
+            raise ValueError("table must be [rows][cap]")
+        rows, cap = table.shape
+        if refs and counts is None:
+            raise ValueError("refs must be [P]")
+        return swarm_cache(self._kinds[dtype], self._at(k, shape, dtype, "k"), self._at(v, shape, dtype, "v"), L, P, H, page, d,
+                           self._at(table, (rows, cap), i32, "table"), self._at(length, (rows,), i32, "length"), self._at(counts, (P,), i32, "refs"), rows, cap)
 
     def tree_attend(self, cache: Cache, layer: int, q, k_new=None, v_new=None, n_new=None, mask=None, sel=None, unit: str = "page",
                     scale: Optional[float] = None, out=None, lse=None, want_lse: bool = False):
@@ -639,93 +637,116 @@ class Swarm:
         tokens of it, and over the drafted tokens that they see.  q [B][T][H*G][d] and k_new, v_new [B][T][H][d] in the cache's
         type; n_new int32 [B]; mask int32 [B][T][ceil(T/32)] words (None: a chain); sel int32 [B][H][n] positions as score_select gives them, of
         pages (unit 'page') or tokens ('token'); scale: d ** -0.5 unless given.  Returns (out [B][T][H*G][d], lse fp32 [B][T][H*G] or None)."""
-        torch = self.torch
         c = self._cache(cache, False)
-        if q.dim() != 4 or q.shape[3] != c.d or q.shape[2] % c.H or not q.shape[2]:
-            raise ValueError(f"q has shape {tuple(q.shape)}, expected [B][T][H*G][d] with H = {c.H} and d = {c.d}")
-        B, T, HG, d = q.shape
-        if unit not in ("page", "token"):
+        shape = q.shape
+        if len(shape) != 4 or shape[3] != c.d or shape[2] % c.H or not shape[2]:
+            raise ValueError(f"q has shape {tuple(shape)}, expected [B][T][H*G][d] with H = {c.H} and d = {c.d}")
+        B, T, HG, d = shape
+        H, kind, i32, at = c.H, cache[0].dtype, self._i32, self._at
+        if unit == "page":
+            per = SWARM_SEL_PAGES
+        elif unit == "token":
+            per = SWARM_SEL_TOKENS
+        else:
             raise ValueError(f"unit is {unit!r}, expected 'page' or 'token'")
-        if sel is not None and sel.dim() != 3:
-            raise ValueError("sel must be [B][H][n]")
+        n = 0
+        if sel is not None:
+            if sel.dim() != 3:
+                raise ValueError("sel must be [B][H][n]")
+            n = sel.shape[2]
+        if mask is not None and mask.dtype is self.torch.uint32:
+            mask = mask.view(i32)
         if out is None:
-            out = torch.empty((B, T, HG, d), dtype=q.dtype, device=self.device)
+            out = self.torch.empty(shape, dtype=kind, device=self.device)
         if lse is None and want_lse:
-            lse = torch.empty((B, T, HG), dtype=torch.float32, device=self.device)
-        kind, words = cache.k.dtype, (torch.int32, torch.uint32)
-        n = 0 if sel is None else sel.shape[2]
-        rc = swarm_tree_attend(self.ctx, c, layer, self._dev(q, kind, "q"), self._opt(k_new, (B, T, c.H, d), kind, "k_new"),
-                               self._opt(v_new, (B, T, c.H, d), kind, "v_new"), B, T, HG // c.H, self._opt(n_new, (B,), torch.int32, "n_new"),
-                               self._opt(mask, (B, T, (T + 31) // 32), words, "mask"), self._opt(sel, (B, c.H, n), torch.int32, "sel"), n,
-                               SWARM_SEL_PAGES if unit == "page" else SWARM_SEL_TOKENS, d ** -0.5 if scale is None else scale,
-                               self._opt(out, q.shape, kind, "out"), self._opt(lse, (B, T, HG), torch.float32, "lse"))
-        self._check("swarm_tree_attend", rc)
+            lse = self.torch.empty((B, T, HG), dtype=self._f32, device=self.device)
+        new = (B, T, H, d)
+        rc = swarm_tree_attend(self.ctx, c, layer, at(q, shape, kind, "q"), at(k_new, new, kind, "k_new"), at(v_new, new, kind, "v_new"), B, T, HG // H,
+                                         at(n_new, (B,), i32, "n_new"), at(mask, (B, T, (T + 31) // 32), i32, "mask"), at(sel, (B, H, n), i32, "sel"), n, per,
+                                         d ** -0.5 if scale is None else scale, at(out, shape, kind, "out"), at(lse, (B, T, HG), self._f32, "lse"))
+        if rc:
+            self._check("swarm_tree_attend", rc)
         return out, lse
 
     def cache_fork(self, cache: Cache, parent, room=None, out=None) -> Cache:
         """Row r goes on as row parent[r] (-1: emptied) with room[r] tokens reserved; parent, room int32 [rows].  Returns the cache with
         its new tables; `out` = (table, length, refs) reuses the caller's tensors (not those of `cache`)."""
-        torch = self.torch
         c = self._cache(cache, True)
-        table, length, refs = out if out is not None else (torch.empty_like(cache.table), torch.empty_like(cache.length), torch.empty_like(cache.refs))
-        rc = swarm_cache_fork(self.ctx, c, self._opt(parent, (c.rows,), torch.int32, "parent"), self._opt(room, (c.rows,), torch.int32, "room"),
-                              self._opt(table, (c.rows, c.cap), torch.int32, "table"), self._opt(length, (c.rows,), torch.int32, "length"),
-                              self._opt(refs, (c.P,), torch.int32, "refs"))
-        self._check("swarm_cache_fork", rc)
-        return dataclasses.replace(cache, table=table, length=length, refs=refs)
+        rows, cap, P, i32, at = c.rows, c.cap, c.P, self._i32, self._at
+        if out is None:
+            new = self.torch.empty(rows * cap + rows + P, dtype=i32, device=self.device)
+            table, length, refs = new[:rows * cap].view(rows, cap), new[rows * cap:rows * cap + rows], new[rows * cap + rows:]
+            base = new.data_ptr()
+            to = base, base + 4 * rows * cap, base + 4 * (rows * cap + rows)
+        else:
+            table, length, refs = out
+            to = at(table, (rows, cap), i32, "table"), at(length, (rows,), i32, "length"), at(refs, (P,), i32, "refs")
+        rc = swarm_cache_fork(self.ctx, c, at(parent, (rows,), i32, "parent"), at(room, (rows,), i32, "room"), *to)
+        if rc:
+            self._check("swarm_cache_fork", rc)
+        return Cache(cache[0], cache[1], table, length, refs)
 
     def cache_append(self, cache: Cache, k_new, v_new, n=None, path=None, out=None) -> Cache:
         """Puts n[b] tokens of each stream (all without n) behind what row b holds, in every layer: token path[b][i], or i without a path.
         k_new, v_new [L][B][T][H][d] in the cache's type; n int32 [B]; path int32 [B][n_max].  Returns the cache with its new lengths;
         `out` = length reuses the caller's tensor (not that of `cache`)."""
-        torch = self.torch
         c = self._cache(cache, False)
-        if k_new.dim() != 5 or path is not None and path.dim() != 2:
+        shape = k_new.shape
+        if len(shape) != 5 or path is not None and path.dim() != 2:
             raise ValueError("k_new and v_new must be [L][B][T][H][d], path [B][n_max]")
-        B, T = k_new.shape[1], k_new.shape[2]
+        B, T = shape[1], shape[2]
         n_max = T if path is None else path.shape[1]
-        kind, shape = cache.k.dtype, (c.L, B, T, c.H, c.d)
-        length = torch.empty_like(cache.length) if out is None else out
-        rc = swarm_cache_append(self.ctx, c, self._opt(k_new, shape, kind, "k_new"), self._opt(v_new, shape, kind, "v_new"), B, T,
-                                self._opt(path, (B, n_max), torch.int32, "path"), n_max, self._opt(n, (B,), torch.int32, "n"),
-                                self._opt(length, (c.rows,), torch.int32, "length"))
-        self._check("swarm_cache_append", rc)
-        return dataclasses.replace(cache, length=length)
+        kind, i32, at, new = cache[0].dtype, self._i32, self._at, (c.L, B, T, c.H, c.d)
+        length = self.torch.empty(c.rows, dtype=i32, device=self.device) if out is None else out
+        rc = swarm_cache_append(self.ctx, c, at(k_new, new, kind, "k_new"), at(v_new, new, kind, "v_new"), B, T, at(path, (B, n_max), i32, "path"), n_max,
+                                          at(n, (B,), i32, "n"), at(length, (c.rows,), i32, "length"))
+        if rc:
+            self._check("swarm_cache_append", rc)
+        return Cache(cache[0], cache[1], cache[2], length, cache[4])
 
     def cache_compact(self, cache: Cache, out=None) -> Tuple[Cache, Any]:
         """Moves the pages in use to the low ids.  Returns (the cache with its new tables, live int32 [1]: how many are in use); `out` =
         (table, refs, live) reuses the caller's tensors (not those of `cache`)."""
-        torch = self.torch
         c = self._cache(cache, True)
-        table, refs, live = out if out is not None else (torch.empty_like(cache.table), torch.empty_like(cache.refs), torch.empty((1,), dtype=torch.int32, device=self.device))
-        rc = swarm_cache_compact(self.ctx, c, self._opt(table, (c.rows, c.cap), torch.int32, "table"), self._opt(refs, (c.P,), torch.int32, "refs"),
-                                 self._opt(live, (1,), torch.int32, "live"))
-        self._check("swarm_cache_compact", rc)
-        return dataclasses.replace(cache, table=table, refs=refs), live
+        rows, cap, P, i32, at = c.rows, c.cap, c.P, self._i32, self._at
+        if out is None:
+            new = self.torch.empty(rows * cap + P + 1, dtype=i32, device=self.device)
+            table, refs, live = new[:rows * cap].view(rows, cap), new[rows * cap:rows * cap + P], new[rows * cap + P:]
+            base = new.data_ptr()
+            to = base, base + 4 * rows * cap, base + 4 * (rows * cap + P)
+        else:
+            table, refs, live = out
+            to = at(table, (rows, cap), i32, "table"), at(refs, (P,), i32, "refs"), at(live, (1,), i32, "live")
+        rc = swarm_cache_compact(self.ctx, c, *to)
+        if rc:
+            self._check("swarm_cache_compact", rc)
+        return Cache(cache[0], cache[1], table, cache[3], refs), live
 
     def beam_select(self, logits, scores, k: int, finished=None, eos: int = -1, vocab: Optional[int] = None, hist=None, step=None, hist_out=None,
                     out=None):
         """The k best continuations of each group: logits [B][K][V] fp32, bf16 or fp16 (the first `vocab` of each row count), scores fp32
         [B][K], finished uint8 [B][K]; hist int32 [B][K][cap], step int32 [1] and hist_out int32 [B][k][cap] reorder the tokens so far.
         Returns (score fp32, parent int32, token int32), each [B][k]; `out` = such a triple reuses the caller's tensors."""
-        torch = self.torch
-        if logits.dim() != 3:
-            raise ValueError("logits must be [B][K][V]")
-        B, K, stride = logits.shape
-        V = stride if vocab is None else vocab
+        shape, dtype = logits.shape, logits.dtype
+        if len(shape) != 3 or dtype not in self._kinds:
+            raise ValueError("logits must be [B][K][V], fp32, bf16 or fp16")
+        B, K, stride = shape
+        i32, f32, at = self._i32, self._f32, self._at
         if out is None:
-            out = (torch.empty((B, k), dtype=torch.float32, device=self.device), torch.empty((B, k), dtype=torch.int32, device=self.device),
-                   torch.empty((B, k), dtype=torch.int32, device=self.device))
+            out = (self.torch.empty((B, k), dtype=f32, device=self.device), self.torch.empty((B, k), dtype=i32, device=self.device),
+                   self.torch.empty((B, k), dtype=i32, device=self.device))
         score, parent, token = out
-        if hist is not None and (hist.dim() != 3 or step is None or hist_out is None):
-            raise ValueError("hist must be [B][K][cap] and comes with step and hist_out")
-        cap = 0 if hist is None else hist.shape[2]
-        rc = swarm_beam_select(self.ctx, self._dev(logits, None, "logits"), self._dtype(logits, "logits", (torch.float32, torch.bfloat16, torch.float16)), stride,
-                               self._opt(scores, (B, K), torch.float32, "scores"), self._opt(finished, (B, K), torch.uint8, "finished"), eos, B, K, V, k,
-                               self._opt(score, (B, k), torch.float32, "score"), self._opt(parent, (B, k), torch.int32, "parent"),
-                               self._opt(token, (B, k), torch.int32, "token"), self._opt(hist, (B, K, cap), torch.int32, "hist"),
-                               self._opt(step, (1,), torch.int32, "step"), cap, self._opt(hist_out, (B, k, cap), torch.int32, "hist_out"))
-        self._check("swarm_beam_select", rc)
+        cap = 0
+        if hist is not None:
+            if hist.dim() != 3 or step is None or hist_out is None:
+                raise ValueError("hist must be [B][K][cap] and comes with step and hist_out")
+            cap = hist.shape[2]
+        rc = swarm_beam_select(self.ctx, at(logits, shape, dtype, "logits"), self._kinds[dtype], stride, at(scores, (B, K), f32, "scores"),
+                                         at(finished, (B, K), self.torch.uint8, "finished"), eos, B, K, stride if vocab is None else vocab, k, at(score, (B, k), f32, "score"),
+                                         at(parent, (B, k), i32, "parent"), at(token, (B, k), i32, "token"), at(hist, (B, K, cap), i32, "hist"), at(step, (1,), i32, "step"),
+                                         cap, at(hist_out, (B, k, cap), i32, "hist_out"))
+        if rc:
+            self._check("swarm_beam_select", rc)
         return out
 
     def calibrate(self, what: int, buf, reps: int = 5) -> float:
