@@ -22,7 +22,8 @@ extern "C" swarm_status swarm_tree_attend(swarm_ctx* ctx, const swarm_cache* cac
     if (sel && (n_sel < 1 || n_sel > (1 << 30) / (unit == SWARM_SEL_PAGES ? cache->page : 1)))
         SWARM_REJECT(ctx, "tree_attend: n_sel=%d below 1, or above 2^30 tokens", n_sel);
     if (sel && unit != SWARM_SEL_PAGES && unit != SWARM_SEL_TOKENS) SWARM_REJECT(ctx, "tree_attend: unknown unit %d", unit);
-    if (!(fabsf(scale) < INFINITY)) SWARM_REJECT(ctx, "tree_attend: scale must be finite");
+    const float scale_log2 = scale * 1.44269504088896341f;
+    if (!(fabsf(scale_log2) < INFINITY)) SWARM_REJECT(ctx, "tree_attend: scale / ln 2 must be finite");
     if (swarm_misaligned(q, 16) || swarm_misaligned(out, 16) || swarm_misaligned(k_new, 16) || swarm_misaligned(v_new, 16) || swarm_misaligned(lse, 4) ||
         swarm_misaligned(n_new, 4) || swarm_misaligned(mask, 4) || swarm_misaligned(sel, 4))
         SWARM_REJECT(ctx, "tree_attend: q, k_new, v_new and out must be 16-byte aligned, the others 4-byte");
@@ -51,7 +52,10 @@ extern "C" swarm_status swarm_tree_attend(swarm_ctx* ctx, const swarm_cache* cac
     if (units > INT32_MAX - 65536) SWARM_REJECT(ctx, "tree_attend: contexts of up to %lld times 128 keys, above 2^31", (long long)units);
     const int resident = 256 * (a.rows <= 4 * RW && (DP <= 128 || a.rows > 16) ? 2 : 1), want = a.tiles < resident ? resident / a.tiles : 1;
     a.parts = (int)(units < want ? units : want);
-    const size_t heads = (4 * ((size_t)B + 1) + 15) / 16 * 16, left = ((size_t)B * cache->H + a.parts) * a.tiles * a.rows;
+    // Scratch for what the parts leave, a slot for each pair and one more for each part.  The parts' share is taken as its bound over all launches
+    // (512 workgroups of up to 128 rows, 256 of up to 256, or one part), which grows with the rows, so that smaller calls never need more.
+    const size_t rows_all = (size_t)a.tiles * a.rows, share = 512 * rows_all < 65536 ? 512 * rows_all : rows_all > 65536 ? rows_all : 65536;
+    const size_t heads = (4 * ((size_t)B + 1) + 15) / 16 * 16, left = (size_t)B * cache->H * rows_all + share;
     st = swarm_scratch(ctx, &ctx->attend, &ctx->attend_bytes, heads + left * (DP + 2) * 4);
     if (st != SWARM_OK) return st;
     a.starts = static_cast<int32_t*>(ctx->attend);
@@ -75,7 +79,7 @@ extern "C" swarm_status swarm_tree_attend(swarm_ctx* ctx, const swarm_cache* cac
     a.flags = ctx->dev_flags;
     a.P = cache->P, a.H = cache->H, a.d = cache->d, a.cap = cache->cap;
     a.B = B, a.T = T, a.G = G, a.n_sel = n_sel, a.unit = unit;
-    a.scale_log2 = scale * 1.44269504088896341f;
+    a.scale_log2 = scale_log2;
     cache->dtype == SWARM_BF16 ? launch_attend_bf16(a, ctx->stream) : launch_attend_fp16(a, ctx->stream);
     return swarm_check_launch(ctx, "attend");
 }

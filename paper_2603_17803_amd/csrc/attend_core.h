@@ -66,6 +66,12 @@ __device__ __forceinline__ float value_of(uint32_t x) {
     if constexpr (BF16) return __uint_as_float(x << 16);
     else return (float)__builtin_bit_cast(_Float16, (uint16_t)x);
 }
+// Two numbers cut to the type.
+template <bool BF16>
+__device__ __forceinline__ uint32_t cut_pair(float lo, float hi) {
+    if constexpr (BF16) return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+    else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(lo, hi));
+}
 template <bool BF16>
 __device__ __forceinline__ int pack(float lo, float hi) { return (int)(bits_of<BF16>(lo) | bits_of<BF16>(hi) << 16); }
 
@@ -130,8 +136,9 @@ __device__ __forceinline__ int quota_of(const attend_args& a, int units) { retur
 
 // What a wave carries of NR * 16 query rows: lane l has row l % 16 of each 16, and of the sums of values the channels
 // 16 c + 4 (l / 16) + 0..3.  KT keys are taken at a time.
-//   TERMS: how many terms of the cache's type a weight enters its product with v as.  Two are a weight to 2^-16 and more,
-//   and cost half as many products again.
+//   TERMS: how many terms of the cache's type a weight enters its product with v as.  Two are a weight to 2^-15 and more, and cost half as
+//   many products again.  The first is cut, not rounded, and the second is what is left and 2^-23 of the weight: neither is negative,
+//   nor 0 where the other is not, so that a value that is infinite stays so.
 template <bool BF16, int DP, int NR, int KT, int TERMS, bool FULL>
 struct flash {
     static constexpr int KS = DP / 32, CT = DP / 16;
@@ -230,9 +237,14 @@ struct flash {
                 }
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    pf[n][0][j][e] = pack<BF16>(p[2 * e], p[2 * e + 1]);
-                    if constexpr (TERMS == 2)
-                        pf[n][1][j][e] = pack<BF16>(p[2 * e] - value_of<BF16>((uint32_t)pf[n][0][j][e] & 0xffffu), p[2 * e + 1] - value_of<BF16>((uint32_t)pf[n][0][j][e] >> 16));
+                    if constexpr (TERMS == 1) {
+                        pf[n][0][j][e] = pack<BF16>(p[2 * e], p[2 * e + 1]);
+                    } else {
+                        constexpr float MORE = 1.f + 0x1p-23f;
+                        const uint32_t cut = cut_pair<BF16>(p[2 * e], p[2 * e + 1]);
+                        pf[n][0][j][e] = (int)cut;
+                        pf[n][1][j][e] = pack<BF16>(__builtin_fmaf(p[2 * e], MORE, -value_of<BF16>(cut & 0xffffu)), __builtin_fmaf(p[2 * e + 1], MORE, -value_of<BF16>(cut >> 16)));
+                    }
                 }
             }
         }
@@ -721,9 +733,10 @@ void launch_attend(const attend_args& a, hipStream_t stream) {
     else if (a.rows == 4 * RW) hipLaunchKernelGGL((attend_wide_kernel<BF16, DP, 4, FULL>), grid, block, 0, stream, a);
     else if (a.rows == 6 * RW) hipLaunchKernelGGL((attend_wide_kernel<BF16, DP, 6, FULL>), grid, dim3(384), 0, stream, a);
     else hipLaunchKernelGGL((attend_wide_kernel<BF16, DP, 8, FULL>), grid, dim3(512), 0, stream, a);
+    constexpr int MANY = DP > 128 ? 4 : 8;      // eight waves would leave wide heads too few registers
     const dim3 rows((unsigned)(a.B * a.H), (unsigned)((a.T * a.G + 15) / 16));
-    if (a.parts <= 4 * a.B * a.H && a.T <= 64) hipLaunchKernelGGL((attend_finish_kernel<BF16, DP, 1, FULL>), rows, dim3(64), 0, stream, a);
-    else hipLaunchKernelGGL((attend_finish_kernel<BF16, DP, 8, FULL>), rows, dim3(512), 0, stream, a);
+    if ((a.parts - 1) / 4 < a.B * a.H && a.T <= 64) hipLaunchKernelGGL((attend_finish_kernel<BF16, DP, 1, FULL>), rows, dim3(64), 0, stream, a);
+    else hipLaunchKernelGGL((attend_finish_kernel<BF16, DP, MANY, FULL>), rows, dim3(64 * MANY), 0, stream, a);
 }
 
 template <bool BF16, int DP>

@@ -491,7 +491,7 @@ extern "C" swarm_status swarm_beam_select(swarm_ctx* ctx, const void* logits, in
     int64_t J = (1024 + (int64_t)rows - 1) / (int64_t)rows;
     J = J < most ? J : most;
     J = J < 64 ? J : 64;
-    const size_t slices = rows * (size_t)J;
+    const size_t slices = rows + 1024;           // rows * J is below, and this grows with the rows: smaller calls never need more
     const swarm_status st = swarm_scratch(ctx, &ctx->beams, &ctx->beams_bytes, slices * (8 + 8 + 4 + 8 * (size_t)k));
     if (st != SWARM_OK) return st;
     beam_args a{};

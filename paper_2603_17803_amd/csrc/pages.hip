@@ -292,7 +292,7 @@ __global__ __launch_bounds__(1024) void fork_one_kernel(fork_args a) {
 __global__ __launch_bounds__(256) void fork_copy_kernel(fork_args a) {
     const int r = blockIdx.x, src = a.copies[3 * r], dst = a.copies[3 * r + 1], piece = a.copies[3 * r + 2] * a.chunks;
     if (src < 0) return;
-    for (int part = blockIdx.y; part < a.L * a.H * 2; part += gridDim.y) {
+    for (int64_t part = blockIdx.y; part < (int64_t)a.L * a.H * 2; part += gridDim.y) {
         v4i* pool = part & 1 ? a.v : a.k;
         const int64_t l = part / 2 / a.H, h = part / 2 % a.H;
         const int64_t from = ((l * a.P + src) * a.H + h) * a.page * a.chunks, to = ((l * a.P + dst) * a.H + h) * a.page * a.chunks;
@@ -420,7 +420,7 @@ __global__ __launch_bounds__(256) void compact_move_kernel(compact_args a) {
     for (int64_t part = blockIdx.x; part < (int64_t)m * a.L * 2; part += gridDim.x) {
         v4i* pool = part & 1 ? a.v : a.k;
         const int64_t l = part / 2 % a.L;
-        const int r = (int)(part / 2 / a.L);
+        const int64_t r = part / 2 / a.L;
         const v4i* from = pool + (l * a.P + a.src[n - m + r]) * piece;
         v4i* to = pool + (l * a.P + a.dst[r]) * piece;
         for (int64_t i = threadIdx.x; i < piece; i += 256) to[i] = from[i];
@@ -523,7 +523,7 @@ swarm_status swarm_cache_fork(swarm_ctx* ctx, const swarm_cache* c, const int32_
         hipLaunchKernelGGL(fork_scan_kernel, dim3(1), dim3(1024), 0, ctx->stream, a);
         hipLaunchKernelGGL(fork_fill_kernel, dim3((unsigned)c->rows), dim3(256), 0, ctx->stream, a);
     }
-    const int parts = 2 * c->L * c->H;
+    const int64_t parts = (int64_t)2 * c->L * c->H;
     hipLaunchKernelGGL(fork_copy_kernel, dim3((unsigned)c->rows, (unsigned)(parts < 64 ? parts : 64)), dim3(256), 0, ctx->stream, a);
     return swarm_check_launch(ctx, "cache_fork");
 }

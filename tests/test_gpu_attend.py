@@ -463,3 +463,99 @@ def test_long_cache_beyond_32_bit_offsets(sw):
     got, _ = sw.tree_attend(b.Cache(k, v, table, torch.tensor(p.lens, dtype=torch.int32, device="cuda")), 0, p.q.cuda(), p.k_new.cuda(), p.v_new.cuda(), lse=got_l)
     torch.cuda.synchronize()
     same(got.cpu(), got_l.cpu(), out, lse, tol_o, tol_l)
+
+
+@pytest.mark.parametrize("d", [136, 192, 256])
+@pytest.mark.parametrize("T,G", [(16, 1), (17, 1), (11, 3), (13, 5), (25, 4), (43, 3), (257 // 8, 8), (130, 2)])
+def test_many_rows_of_wide_heads(sw, d, T, G):
+    Problem(d + T, "fp16" if T % 2 else "bf16", 2, T, 1, G, d, 16, [203, 40], tree=True).check(sw)
+
+
+@pytest.mark.parametrize("T,G", [(3, 11), (13, 5), (32, 4), (43, 3), (75, 2), (49, 4), (65, 4), (97, 4)])
+@pytest.mark.parametrize("d", [72, 128])
+def test_many_rows_over_several_parts(sw, d, T, G):
+    """Rows of one to eight waves and of two tiles, streams that end at every place of a part."""
+    Problem(d + T, "bf16" if T % 2 else "fp16", 4, T, 2, G, d, 16, [385, 0, 64, 129], tree=True, n_new=[T, T, max(1, T - 3), 2]).check(sw)
+
+
+@pytest.mark.parametrize("B", [63, 64, 65, 130, 256, 257, 600])
+@pytest.mark.parametrize("T,G", [(1, 2), (20, 2)])
+def test_many_streams(sw, B, T, G):
+    """Streams that are found by one wave, by one pass and by two, among them empty ones and ones without drafted tokens."""
+    rng = np.random.default_rng(B)
+    lens = [int(x) for x in rng.choice([0, 1, 20, 128, 129, 300], size=B)]
+    Problem(B, "bf16", B, T, 1, G, 32, 16, lens, n_new=[int(x) for x in rng.choice([0, 1, T], size=B)]).check(sw)
+
+
+def test_values_that_are_not_numbers_stay_in_their_stream(sw):
+    """A token of the context is seen by its stream and head alone."""
+    for T, G in ((2, 2), (20, 3)):
+        p = Problem(24 + T, "bf16", 3, T, 2, G, 64, 16, [300, 200, 30], tree=True)
+        out, lse, tol_o, tol_l = p.reference()
+        p.v[0, int(p.table[1, 3]), 1, 5, 7] = math.nan
+        p.v[0, int(p.table[1, 8]), 1, 2, 9] = math.inf
+        got, got_l = p.run(sw)
+        hit = got[1, :, G:]
+        assert hit[..., 7].isnan().all() and (hit[..., 9] == math.inf).all()
+        got[1, :, G:, 7], got[1, :, G:, 9] = 77.0, 77.0
+        out[1, :, G:, 7], out[1, :, G:, 9] = 77.0, 77.0
+        same(got, got_l, out, lse, tol_o, tol_l)
+        p.k[0, int(p.table[1, 3]), 1, 5, 7] = math.nan
+        got, got_l = p.run(sw)
+        assert got[1, :, G:].isnan().all() and got_l[1, :, G:].isnan().all()
+        keep = [0, 2]
+        same(got[keep], got_l[keep], out[keep], lse[keep], tol_o[keep], tol_l[keep])
+
+
+def test_smaller_calls_are_recorded_after_a_larger_one(sw):
+    """No call with fewer streams, tokens or query heads, or narrower heads, needs more scratch than the larger one before it."""
+    from paper_2603_17803_amd import binding as b
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        for big, small in [((2, 48, 2, 4, 128), [(2, 32, 2, 4, 128), (1, 48, 2, 4, 128), (2, 16, 1, 4, 128), (2, 48, 2, 1, 128), (2, 1, 2, 4, 128), (2, 33, 2, 4, 64)]),
+                           ((1, 65, 1, 4, 128), [(1, 64, 1, 4, 128), (1, 32, 1, 4, 128), (1, 8, 1, 4, 128)]),
+                           ((1, 40, 1, 4, 256), [(1, 40, 1, 4, 192), (1, 33, 1, 4, 128), (1, 32, 1, 4, 256), (1, 8, 1, 2, 256), (1, 40, 1, 4, 64)])]:
+            s = b.Swarm(0, stream=stream)
+            Problem(1, "bf16", *big, 16, [5000] * big[0]).run(s)
+            for shape in small:
+                p = Problem(2, "bf16", *shape, 16, [5000] * shape[0])
+                dev = [x.cuda() for x in (p.k, p.v, torch.from_numpy(p.table), torch.tensor(p.lens, dtype=torch.int32), p.q, p.k_new, p.v_new)]
+                out = torch.zeros_like(dev[4])
+                stream.synchronize()
+                s.capture_begin()
+                s.tree_attend(b.Cache(*dev[:4]), 0, *dev[4:], scale=p.scale, out=out)
+                graph = s.capture_end()
+                for _ in range(2):
+                    out.zero_()
+                    s.graph_launch(graph)
+                    stream.synchronize()
+                    assert torch.equal(out.cpu(), p.run(s)[0])
+                b.swarm_graph_destroy(graph)
+            s.close()
+
+
+def test_contexts_on_two_streams_at_once(sw):
+    from paper_2603_17803_amd import binding as b
+    made = []
+    for i, T in enumerate((1, 24)):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            p = Problem(30 + i, "bf16", 2, T, 2, 4, 128, 16, [4000, 900])
+            dev = [x.cuda() for x in (p.k, p.v, torch.from_numpy(p.table), torch.tensor(p.lens, dtype=torch.int32), p.q, p.k_new, p.v_new)]
+            made.append((b.Swarm(0, stream=stream), dev, [torch.zeros_like(dev[4]) for _ in range(20)], p.run(sw)[0]))
+    torch.cuda.synchronize()
+    for i in range(20):
+        for s, dev, outs, _ in made:
+            s.tree_attend(b.Cache(*dev[:4]), 0, *dev[4:], out=outs[i])
+    torch.cuda.synchronize()
+    for s, _, outs, want in made:
+        assert all(torch.equal(o.cpu(), want) for o in outs)
+        s.close()
+
+
+def test_scale_that_fp32_does_not_hold_in_units_of_ln_2(sw):
+    from paper_2603_17803_amd import binding as b
+    p = Problem(40, "bf16", 1, 1, 1, 1, 64, 16, [3])
+    p.scale = 3e38
+    with pytest.raises(b.SwarmError):
+        p.run(sw)

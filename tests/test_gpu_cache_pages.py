@@ -380,3 +380,13 @@ def test_recorded_and_captured_steps_replay(sw):
         del captured
         stream.synchronize()
         s.close()
+
+
+@pytest.mark.parametrize("rows,P,cap", [(16, 8192, 256), (16, 4200, 257), (64, 8193, 64), (65, 8192, 64), (32, 5000, 128), (33, 5000, 128), (48, 3200, 65), (1024, 8192, 1), (2, 500, 200)])
+def test_fork_by_one_workgroup_and_by_several(sw, rows, P, cap):
+    """Either side of the sizes that one workgroup plans by itself, rows of any length, more children than pages for some."""
+    h = Host(rows + cap, L=1, H=1, d=8, page=2, P=P, rows=rows, cap=cap)
+    h.fill([int(x) for x in h.rng.integers(0, 2 * min(cap, P // rows) + 1, size=rows)])
+    fork(sw, h, h.rng.integers(-1, rows, size=rows), h.rng.integers(0, 5, size=rows))
+    fork(sw, h, h.rng.integers(0, max(1, rows // 4), size=rows), h.rng.integers(0, 9, size=rows))
+    sw.device_status()
