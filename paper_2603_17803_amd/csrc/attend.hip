@@ -36,21 +36,17 @@ extern "C" swarm_status swarm_tree_attend(swarm_ctx* ctx, const swarm_cache* cac
     if (swarm_overlap(outs, 2, ins, 10)) SWARM_REJECT(ctx, "tree_attend: out or lse overlaps an input, or the other");
 
     attend_args a{};
-    // As many rows as a wave takes go to the kernel whose waves have keys of their own, more to the one whose waves share them: as few tiles of
-    // rows as 8 waves allow, and in each as few waves as the rows need, in pairs.
-    const int M = T * G, DP = attend_width(cache->d), RW = attend_wave_rows(DP);
-    if (M <= RW) {
-        a.tiles = 1;
-        a.rows = (M + 15) / 16 * 16;
-    } else {
-        a.tiles = (M + 8 * RW - 1) / (8 * RW);
-        a.rows = (M + 2 * RW * a.tiles - 1) / (2 * RW * a.tiles) * 2 * RW;
-    }
+    // Up to 32 rows (16 of heads wider than 128, which take more registers) go to the kernel whose waves have keys of their own, more to the one whose waves
+    // share them: as few tiles of up to 256 (128) rows as they need, and in each the smallest of that kernel's forms.
+    const int M = T * G, DP = attend_width(cache->d), most = DP > 128 ? 128 : 256;
+    a.tiles = (M + most - 1) / most;
+    const int each = (M + a.tiles - 1) / a.tiles;
+    a.rows = each <= 16 ? 16 : each <= 32 ? 32 : each <= 64 ? 64 : each <= 96 && DP > 128 ? 96 : each <= 128 ? 128 : each <= 192 ? 192 : 256;
     // as many parts as workgroups are resident at once, and no more than there can be units
     const int64_t slots = !sel ? (int64_t)cache->cap * cache->page : unit == SWARM_SEL_PAGES ? (int64_t)n_sel * cache->page : n_sel;
     const int64_t units = (int64_t)B * cache->H * ((slots + ATTEND_UNIT - 1) / ATTEND_UNIT);
     if (units > INT32_MAX - 65536) SWARM_REJECT(ctx, "tree_attend: contexts of up to %lld times 128 keys, above 2^31", (long long)units);
-    const int resident = 256 * (a.rows <= 4 * RW && (DP <= 128 || a.rows > 16) ? 2 : 1), want = a.tiles < resident ? resident / a.tiles : 1;
+    const int resident = 256 * ((DP <= 128 ? a.rows <= 128 : a.rows > 16 && a.rows <= 64) ? 2 : 1), want = a.tiles < resident ? resident / a.tiles : 1;
     a.parts = (int)(units < want ? units : want);
     // Scratch for what the parts leave, a slot for each pair and one more for each part.  The parts' share is taken as its bound over all launches
     // (512 workgroups of up to 128 rows, 256 of up to 256, or one part), which grows with the rows, so that smaller calls never need more.

@@ -32,8 +32,7 @@ struct attend_args {
 
 // Head dimension that the kernels work with: the next of five.
 inline int attend_width(int d) { return d <= 64 ? 64 : d <= 96 ? 96 : d <= 128 ? 128 : d <= 192 ? 192 : 256; }
-constexpr int attend_wave_rows(int DP) { return DP > 128 ? 16 : 32; }   // rows of a wave of the kernel for many rows: what its sums leave room for in half of the register file
-constexpr int ATTEND_UNIT = 128;                                       // keys of a unit of the line
+constexpr int ATTEND_UNIT = 128;                 // keys of a unit of the line
 
 void launch_attend_bf16(const attend_args& a, hipStream_t stream);
 void launch_attend_fp16(const attend_args& a, hipStream_t stream);
@@ -57,11 +56,6 @@ __device__ __forceinline__ v4f mfma(v4i x, v4i y, v4f c) {
     else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(hf8, x), __builtin_bit_cast(hf8, y), c, 0, 0, 0);
 }
 template <bool BF16>
-__device__ __forceinline__ uint32_t bits_of(float x) {
-    if constexpr (BF16) return __builtin_bit_cast(uint16_t, (__bf16)x);
-    else return __builtin_bit_cast(uint16_t, (_Float16)x);
-}
-template <bool BF16>
 __device__ __forceinline__ float value_of(uint32_t x) {
     if constexpr (BF16) return __uint_as_float(x << 16);
     else return (float)__builtin_bit_cast(_Float16, (uint16_t)x);
@@ -72,8 +66,15 @@ __device__ __forceinline__ uint32_t cut_pair(float lo, float hi) {
     if constexpr (BF16) return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
     else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(lo, hi));
 }
+// Two numbers rounded to it, in one instruction.  (Rounded one by one: 192 rows of 96 73 us, so: 70.)
 template <bool BF16>
-__device__ __forceinline__ int pack(float lo, float hi) { return (int)(bits_of<BF16>(lo) | bits_of<BF16>(hi) << 16); }
+__device__ __forceinline__ int pack(float lo, float hi) {
+    typedef float v2f __attribute__((ext_vector_type(2)));
+    typedef __bf16 v2b __attribute__((ext_vector_type(2)));
+    typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+    if constexpr (BF16) return __builtin_bit_cast(int, __builtin_convertvector((v2f{lo, hi}), v2b));
+    else return __builtin_bit_cast(int, __builtin_convertvector((v2f{lo, hi}), v2h));
+}
 
 // Maximum and sum over the four lanes (l, l + 16, l + 32, l + 48) that share a query row.
 __device__ __forceinline__ float rows_max(float x) {
@@ -495,12 +496,16 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attend_context_kernel(a
     }
 }
 
-// The same for many rows: W waves share tiles of KT keys in LDS, K and V, two of them: while one is worked on, the next comes into
-// registers, and from there into the other's place.  The matrix cores bound it, so a weight enters its product with v as one term of the cache's
-// type: off by half a step at most, as the result is by its own rounding.  (Two terms: 131000 tokens x 256 rows x 8 heads 243 us, one: 186.)
-template <bool BF16, int DP, int W, bool FULL>
-__global__ __launch_bounds__(64 * W, W <= 4 ? 2 : 1) void attend_wide_kernel(attend_args a) {
-    constexpr int NR = attend_wave_rows(DP) / 16, ROWS = 16 * NR * W, KT = DP > 128 || W == 2 ? 32 : 64, THREADS = 64 * W;
+// The same for many rows: W waves of NR * 16 share tiles of KT keys in LDS, K and V, two of them: while one is worked on, the next comes into
+// registers, and from there into the other's place.  The vector units bound it (the exponentials and their sums, and the matrix cores' work on top), so a
+// weight enters its product with v as one term of the cache's type: off by half a step at most, as the result is by its own rounding.  (Two terms: 131000
+// tokens x 256 rows x 8 heads 243 us, one: 186.)
+// Which form takes how many rows is measured.  Heads of 128 / 64, 96 pairs of 700 to 6000 tokens: 64 rows by four waves of 16 51 / 32 us, by two of 32
+// 61 / 42; 96 rows by four of 32 66 / 43, by six of 16 78 / 44; 128 rows by four of 32 71 / 46, by eight of 16 81 / 48; 192 rows by twelve of 16 77 / 50,
+// by six of 32 81 / 54.  8 pairs of 131000 tokens, heads of 128: 256 rows by eight of 32 215, by sixteen of 16 235.
+template <bool BF16, int DP, int W, int NR, bool FULL>
+__global__ __launch_bounds__(64 * W, DP > 128 ? (W == 4 ? 2 : 1) : W * (16 * NR * W <= 128 ? 2 : 1) / 4) void attend_wide_kernel(attend_args a) {
+    constexpr int ROWS = 16 * NR * W, KT = DP > 128 ? 32 : 64, THREADS = 64 * W;
     typedef flash<BF16, DP, NR, KT, 1, FULL> state;
     constexpr int KLD = DP + 8, VLD = state::VLD;     // LDS rows: 16 rows' pieces of 16 bytes meet no bank twice
     constexpr int LPR = DP / 8, PIECES = KT * LPR, MINE = (PIECES + THREADS - 1) / THREADS;
@@ -726,13 +731,19 @@ __global__ __launch_bounds__(64 * W, DP > 128 ? 1 : 2) void attend_finish_kernel
 template <bool BF16, int DP, bool FULL>
 void launch_attend(const attend_args& a, hipStream_t stream) {
     const dim3 grid((unsigned)((a.parts + 7) / 8 * 8 * a.tiles)), block(256);
-    constexpr int RW = attend_wave_rows(DP);
     if (a.rows == 16) hipLaunchKernelGGL((attend_context_kernel<BF16, DP, 1, FULL>), grid, block, 0, stream, a);
-    else if (RW == 32 && a.rows == 32) hipLaunchKernelGGL((attend_context_kernel<BF16, DP, RW / 16, FULL>), grid, block, 0, stream, a);
-    else if (a.rows == 2 * RW) hipLaunchKernelGGL((attend_wide_kernel<BF16, DP, 2, FULL>), grid, dim3(128), 0, stream, a);
-    else if (a.rows == 4 * RW) hipLaunchKernelGGL((attend_wide_kernel<BF16, DP, 4, FULL>), grid, block, 0, stream, a);
-    else if (a.rows == 6 * RW) hipLaunchKernelGGL((attend_wide_kernel<BF16, DP, 6, FULL>), grid, dim3(384), 0, stream, a);
-    else hipLaunchKernelGGL((attend_wide_kernel<BF16, DP, 8, FULL>), grid, dim3(512), 0, stream, a);
+    else if constexpr (DP <= 128) {
+        if (a.rows == 32) hipLaunchKernelGGL((attend_context_kernel<BF16, DP, 2, FULL>), grid, block, 0, stream, a);
+        else if (a.rows == 64) hipLaunchKernelGGL((attend_wide_kernel<BF16, DP, 4, 1, FULL>), grid, block, 0, stream, a);
+        else if (a.rows == 128) hipLaunchKernelGGL((attend_wide_kernel<BF16, DP, 4, 2, FULL>), grid, block, 0, stream, a);
+        else if (a.rows == 192) hipLaunchKernelGGL((attend_wide_kernel<BF16, DP, 12, 1, FULL>), grid, dim3(768), 0, stream, a);
+        else hipLaunchKernelGGL((attend_wide_kernel<BF16, DP, 8, 2, FULL>), grid, dim3(512), 0, stream, a);
+    } else {
+        if (a.rows == 32) hipLaunchKernelGGL((attend_wide_kernel<BF16, DP, 2, 1, FULL>), grid, dim3(128), 0, stream, a);
+        else if (a.rows == 64) hipLaunchKernelGGL((attend_wide_kernel<BF16, DP, 4, 1, FULL>), grid, block, 0, stream, a);
+        else if (a.rows == 96) hipLaunchKernelGGL((attend_wide_kernel<BF16, DP, 6, 1, FULL>), grid, dim3(384), 0, stream, a);
+        else hipLaunchKernelGGL((attend_wide_kernel<BF16, DP, 8, 1, FULL>), grid, dim3(512), 0, stream, a);
+    }
     constexpr int MANY = DP > 128 ? 4 : 8;      // eight waves would leave wide heads too few registers
     const dim3 rows((unsigned)(a.B * a.H), (unsigned)((a.T * a.G + 15) / 16));
     if ((a.parts - 1) / 4 < a.B * a.H && a.T <= 64) hipLaunchKernelGGL((attend_finish_kernel<BF16, DP, 1, FULL>), rows, dim3(64), 0, stream, a);
