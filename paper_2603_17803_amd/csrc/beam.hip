@@ -2,9 +2,10 @@
 //
 // One pass over the logits.  A beam's best k tokens and its normaliser ln sum exp x come from one read: a workgroup takes a slice of a
 // row in chunks of 4096 logits, holds a lower bound of the slice's k-th best logit, and puts the few that exceed it into a list in LDS, which is
-// cut down to its k best whenever it has grown.  The first bound is the k-th largest of the 256 threads' own maxima of the first chunk.  Between
-// two slices' ends a logit costs its exponential, one comparison and one addition.  What bounds it is memory for fp32 and about as much
-// the vector units for 16-bit logits (8 of them in 16 bytes, 8 exponentials at a quarter of the rate).
+// cut down to its k best whenever it has grown.  The first bound is the k-th largest of the first chunk's maxima of 64 groups of threads (of 256 threads for
+// k above 32).  A logit costs its exponential, one comparison and one addition.  What bounds it is memory for fp32 (512 rows of 128000, k = 1: 52 us
+// with the second kernel, 5.0 TB/s), and with 16-bit logits the candidates: without the few that each chunk adds after the first, and the waits of
+// the other waves for the one that adds them, k = 16 takes 42 us in place of 54; the exponentials cost nothing.
 //
 // A second kernel, a workgroup for each group of beams, merges the sorted lists one candidate at a time and moves the histories.
 #include <math.h>
@@ -71,6 +72,7 @@ __device__ __forceinline__ float widen(uint32_t bits) {
 // How many of n keys in LDS are above `key`; n is rounded up to a multiple of 2 by zeros.
 __device__ __forceinline__ int above(const u64* keys, int n, u64 key) {
     int c = 0;
+#pragma unroll 8
     for (int i = 0; i < n; i += 2) {
         const ulonglong2 x = *reinterpret_cast<const ulonglong2*>(keys + i);
         c += x.x > key;
@@ -504,7 +506,8 @@ extern "C" swarm_status swarm_beam_select(swarm_ctx* ctx, const void* logits, in
     a.refs = reinterpret_cast<double*>(a.lists + slices * k);
     a.found = reinterpret_cast<int32_t*>(a.refs + slices);
     a.eos = eos, a.K = K, a.V = V, a.k = k, a.hist_cap = hist_cap, a.J = (int)J, a.per = (int)((vectors + J - 1) / J);
-    a.trim = 4 * k < 48 ? 48 : 4 * k;            // 512 at most
+    // Cutting a list costs barriers and gives a higher bound: 512 rows of 128001 bf16 logits, k = 16 (32): at 48 (96) candidates 54 us (66), at 64 (128) 55 (69).
+    a.trim = 3 * k < 48 ? 48 : 3 * k;            // below 512
     if (dtype == SWARM_FP32) launch_beams<SWARM_FP32>(a, (int64_t)rows, ctx->stream);
     else if (dtype == SWARM_BF16) launch_beams<SWARM_BF16>(a, (int64_t)rows, ctx->stream);
     else launch_beams<SWARM_FP16>(a, (int64_t)rows, ctx->stream);
