@@ -657,7 +657,7 @@ class Swarm:
         if mask is not None and mask.dtype is self.torch.uint32:
             mask = mask.view(i32)
         if out is None:
-            out = self.torch.empty(shape, dtype=kind, device=self.device)
+            out = self.torch.empty_like(q)
         if lse is None and want_lse:
             lse = self.torch.empty((B, T, HG), dtype=self._f32, device=self.device)
         new = (B, T, H, d)
@@ -674,10 +674,9 @@ class Swarm:
         c = self._cache(cache, True)
         rows, cap, P, i32, at = c.rows, c.cap, c.P, self._i32, self._at
         if out is None:
-            new = self.torch.empty(rows * cap + rows + P, dtype=i32, device=self.device)
-            table, length, refs = new[:rows * cap].view(rows, cap), new[rows * cap:rows * cap + rows], new[rows * cap + rows:]
-            base = new.data_ptr()
-            to = base, base + 4 * rows * cap, base + 4 * (rows * cap + rows)
+            like = self.torch.empty_like
+            table, length, refs = like(cache[2]), like(cache[3]), like(cache[4])
+            to = table.data_ptr(), length.data_ptr(), refs.data_ptr()
         else:
             table, length, refs = out
             to = at(table, (rows, cap), i32, "table"), at(length, (rows,), i32, "length"), at(refs, (P,), i32, "refs")
@@ -697,7 +696,7 @@ class Swarm:
         B, T = shape[1], shape[2]
         n_max = T if path is None else path.shape[1]
         kind, i32, at, new = cache[0].dtype, self._i32, self._at, (c.L, B, T, c.H, c.d)
-        length = self.torch.empty(c.rows, dtype=i32, device=self.device) if out is None else out
+        length = self.torch.empty_like(cache[3]) if out is None else out
         rc = swarm_cache_append(self.ctx, c, at(k_new, new, kind, "k_new"), at(v_new, new, kind, "v_new"), B, T, at(path, (B, n_max), i32, "path"), n_max,
                                           at(n, (B,), i32, "n"), at(length, (c.rows,), i32, "length"))
         if rc:
@@ -710,10 +709,8 @@ class Swarm:
         c = self._cache(cache, True)
         rows, cap, P, i32, at = c.rows, c.cap, c.P, self._i32, self._at
         if out is None:
-            new = self.torch.empty(rows * cap + P + 1, dtype=i32, device=self.device)
-            table, refs, live = new[:rows * cap].view(rows, cap), new[rows * cap:rows * cap + P], new[rows * cap + P:]
-            base = new.data_ptr()
-            to = base, base + 4 * rows * cap, base + 4 * (rows * cap + P)
+            table, refs, live = self.torch.empty_like(cache[2]), self.torch.empty_like(cache[4]), self.torch.empty(1, dtype=i32, device=self.device)
+            to = table.data_ptr(), refs.data_ptr(), live.data_ptr()
         else:
             table, refs, live = out
             to = at(table, (rows, cap), i32, "table"), at(refs, (P,), i32, "refs"), at(live, (1,), i32, "live")
