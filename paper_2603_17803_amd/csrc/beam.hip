@@ -333,41 +333,60 @@ __global__ __launch_bounds__(1024) void beam_join_kernel(beam_args a) {
     __shared__ double norm[64];                  // ln sum exp of each beam's logits; of a finished one nothing
     __shared__ float base[64];
     __shared__ uint8_t head[MOST_LISTS], length[MOST_LISTS], beams[MOST_LISTS];   // where each list stands, its candidates (255: the one of a finished beam), its beam
-    __shared__ u64 staged[STAGED];
+    __shared__ u64 staged[STAGED], scored[STAGED];   // candidates, and their scores
     __shared__ int parent[128], token[128];
+    __shared__ float best[128];
     const int64_t b = blockIdx.x;
     const int t = threadIdx.x, lists = a.K * a.J, n_staged = lists * a.k <= STAGED ? lists * a.k : 0;
     for (int i = t; i < lists; i += 1024) head[i] = 0, length[i] = (uint8_t)a.found[b * lists + i], beams[i] = (uint8_t)(i / a.J);
     for (int i = t; i < n_staged; i += 1024) staged[i] = a.lists[b * lists * a.k + i];
-    if (t < a.K) {
-        base[t] = a.scores[b * a.K + t];
-        const int64_t at = (b * a.K + t) * a.J;
-        double big = -INFINITY, z = 0.0;
-        if (a.found[at] >= 0) {
-            for (int j = 0; j < a.J; ++j) big = fmax(big, a.refs[at + j]);
-            for (int j = 0; j < a.J; ++j) z += a.sums[at + j] * exp2(a.refs[at + j] - big);
+    int step = a.hist ? a.step[0] : 0;
+    {
+        // 16 lanes a beam, four of its up to 64 slices each
+        const int beam = t / 16, lane = t % 16;
+        const int64_t at = (b * a.K + beam) * a.J;
+        double ref[4], sum[4], big = -INFINITY, z = 0.0;
+        const bool live = beam < a.K && a.found[at] >= 0;
+        for (int i = 0; i < 4; ++i) {
+            const bool there = live && lane + 16 * i < a.J;
+            ref[i] = there ? a.refs[at + lane + 16 * i] : -INFINITY;
+            sum[i] = there ? a.sums[at + lane + 16 * i] : 0.0;
+            big = fmax(big, ref[i]);
         }
-        norm[t] = big * 0.69314718055994530942 + log(z);
+        for (int o = 8; o; o >>= 1) big = fmax(big, __shfl_xor(big, o, 16));
+        for (int i = 0; i < 4; ++i)
+            if (lane + 16 * i < a.J) z += sum[i] * exp2(ref[i] - big);
+        for (int o = 8; o; o >>= 1) z += __shfl_xor(z, o, 16);
+        if (beam < a.K && lane == 0) {
+            base[beam] = a.scores[b * a.K + beam];
+            norm[beam] = big * 0.69314718055994530942 + log(z);
+        }
+    }
+    __syncthreads();
+    auto score_of_key = [&](int beam, u64 c, bool finished) {
+        double x = base[beam];
+        if (!finished) x += (double)logit_of(c) - norm[beam];
+        return ordered(x != x ? (double)-INFINITY : x);
+    };
+    for (int i = t; i < n_staged; i += 1024) {
+        const int list = i / a.k;
+        if (i - list * a.k < length[list] && length[list] != 255) scored[i] = score_of_key(beams[list], staged[i], false);
     }
     __syncthreads();
     if (t < 64) {
         // The lane's best candidate (score 0: none), its beam and its list; where it has one list alone, the candidate behind it too.
-        u64 score = 0, key = 0, behind = 0;
+        u64 score = 0, key = 0, behind = 0, behind_score = 0;
         int owner = 0, mine = t, at = 0, n = 0;
         const bool single = lists <= 64;
         auto key_of = [&](int list, int place) { return n_staged ? staged[list * a.k + place] : a.lists[(b * lists + list) * a.k + place]; };
-        auto score_of_key = [&](int beam, u64 c, bool finished) {
-            double x = base[beam];
-            if (!finished) x += (double)logit_of(c) - norm[beam];
-            return ordered(x != x ? (double)-INFINITY : x);
-        };
+        auto score_at = [&](int list, int place, int beam, u64 c) { return n_staged ? scored[list * a.k + place] : score_of_key(beam, c, false); };
         auto refresh = [&]() {
             score = 0;
             for (int i = t; i < lists; i += 64) {
                 const int beam = beams[i], count = length[i], place = head[i];
                 const bool finished = count == 255;
                 if (place >= (finished ? 1 : count)) continue;
-                const u64 c = finished ? candidate(0.f, a.eos) : key_of(i, place), s = score_of_key(beam, c, finished);
+                const u64 c = finished ? candidate(0.f, a.eos) : key_of(i, place), s = finished ? score_of_key(beam, c, true) : score_at(i, place, beam, c);
                 // lists come in the order of beams, a beam's in the order of its slices
                 if (s > score || (s == score && beam == owner && c > key)) score = s, key = c, mine = i, owner = beam;
             }
@@ -375,7 +394,7 @@ __global__ __launch_bounds__(1024) void beam_join_kernel(beam_args a) {
         refresh();
         if (single && t < lists) {
             n = length[t] == 255 ? 1 : length[t];
-            if (n > 1) behind = key_of(t, 1);
+            if (n > 1) behind = key_of(t, 1), behind_score = score_at(t, 1, owner, behind);
         }
         for (int i = 0; i < a.k; ++i) {
             // the largest score, then the lowest beam, the largest logit, the lowest token
@@ -388,7 +407,7 @@ __global__ __launch_bounds__(1024) void beam_join_kernel(beam_args a) {
                 who = __ballot(in);
             }
             if (hi == ~0u) {
-                if (t == 0) parent[i] = -1, token[i] = -1, a.out_score[b * a.k + i] = -INFINITY;
+                if (t == 0) parent[i] = -1, token[i] = -1, best[i] = -INFINITY;
                 continue;
             }
             if (who & (who - 1)) {
@@ -403,12 +422,12 @@ __global__ __launch_bounds__(1024) void beam_join_kernel(beam_args a) {
             if (t == __ffsll((long long)who) - 1) {
                 parent[i] = (int)(b * a.K) + owner;
                 token[i] = token_of(key);
-                a.out_score[b * a.k + i] = (float)score_of(score);
+                best[i] = (float)score_of(score);
                 if (single) {
                     ++at;
                     key = behind;
-                    score = at < n ? score_of_key(owner, key, false) : 0;
-                    if (at + 1 < n) behind = key_of(t, at + 1);
+                    score = at < n ? behind_score : 0;
+                    if (at + 1 < n) behind = key_of(t, at + 1), behind_score = score_at(t, at + 1, owner, behind);
                 } else {
                     ++head[mine];
                     refresh();
@@ -417,9 +436,8 @@ __global__ __launch_bounds__(1024) void beam_join_kernel(beam_args a) {
         }
     }
     __syncthreads();
-    for (int i = t; i < a.k; i += 1024) a.out_parent[b * a.k + i] = parent[i], a.out_token[b * a.k + i] = token[i];
+    for (int i = t; i < a.k; i += 1024) a.out_parent[b * a.k + i] = parent[i], a.out_token[b * a.k + i] = token[i], a.out_score[b * a.k + i] = best[i];
     if (!a.hist) return;
-    int step = a.step[0];
     const bool fits = step >= 0 && step < a.hist_cap;
     if (!fits) {
         if (t == 0) atomicOr(a.flags, SWARM_DEV_BAD_ENTRY);
