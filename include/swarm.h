@@ -409,9 +409,10 @@ typedef struct {
  *   (SWARM_SEL_PAGES, positions in the row's table), or those tokens themselves (SWARM_SEL_TOKENS, positions in the row).
  * A token that sees nothing, or scores of -inf only, gets out = 0 and lse = -inf.  lse joins attention over parts: entries that come
  * in later (from an SSD) are attended over in a call of their own, and the two results weighted by exp(lse - joint lse).
- * Products and sums are fp32; a weight enters its product with v as two terms of the cache's type (about 16 bits, so that the result
- * is rounded once, at the end), the sum of weights in fp32.  What a token does not see never reaches its result, infinities
- * and NaN included.
+ * Products and sums are fp32, the sum of weights that of the fp32 weights.  A weight enters its product with v as two terms of the cache's type
+ * (15 bits and more, so that the result is rounded once, at the end) where T*G <= 32 (16 for d > 128), and for the drafted tokens always; a
+ * weight of the context beyond that is rounded to the type (off by half a step, as the result is by its own rounding).  What a token does not
+ * see never reaches its result, infinities and NaN included.
  *
  * layer        which of the cache's L layers.
  * q            device, [B][T][H*G][d] in the cache's type, 16-byte aligned.   B <= rows streams, T drafted tokens each (1..256; one
@@ -424,7 +425,7 @@ typedef struct {
  *              NULL: a chain, token i sees the tokens 0..i.
  * sel          device, int32 [B][H][n_sel] or NULL.  -1 is padding; entries should be distinct (one that is listed twice counts
  *              twice); what lies behind the row's tokens counts for nothing.   unit: swarm_sel_unit.
- * scale        a finite number.
+ * scale        a number whose product with 1 / ln 2 is finite in fp32.
  * out          device, [B][T][H*G][d] in the cache's type, 16-byte aligned.   lse: device, fp32 [B][T][H*G], or NULL.
  * A page id outside [0,P) drops its tokens (SWARM_DEV_BAD_PAGE); a selected position outside [-1, cap) or [-1, cap * page) is
  * dropped (SWARM_DEV_BAD_ENTRY); a length outside [0, cap * page], or n_new outside [0, T], is cut to it (SWARM_DEV_BAD_LEN).
@@ -520,8 +521,8 @@ swarm_status swarm_beam_select(swarm_ctx* ctx, const void* logits, int32_t dtype
  * context's scratch: once a context has recorded, scratch that later calls outgrow is kept (not
  * freed) until swarm_destroy, so earlier graphs stay replayable; destroy graphs before their context.
  * (A graph that the caller captures by its own means is known to the context only where a call in it
- * takes one of the shorter ways that have scratch of their own: other ones are replayable until a later
- * call outgrows scratch that they refer to.)
+ * is one of swarm_tree_attend, swarm_cache_* and swarm_beam_select, or takes one of the shorter ways that
+ * have scratch of their own: other ones are replayable until a later call outgrows scratch that they refer to.)
  */
 typedef struct swarm_graph swarm_graph;
 swarm_status swarm_capture_begin(swarm_ctx* ctx);

@@ -1,15 +1,16 @@
 // Attention of drafted tokens over a paged cache.
 //
 // The T*G query rows that a KV head's group has (drafted token i, query head g: row i*G + g) share every key and value, so a
-// workgroup takes up to 64 of them and streams the keys past: per 16 rows, S^T = K Q^T on the 16x16x32 matrix instruction (keys are
+// workgroup takes up to 256 of them and streams the keys past: per 16 rows, S^T = K Q^T on the 16x16x32 matrix instruction (keys are
 // the rows of its result, query rows its columns), the softmax's running maximum and sum a lane per query row, O^T += V^T P^T on the
 // same instruction.  A lane's eight weights of 32 keys are, as they come out of the first product, one operand of the
-// second; V^T's operand is read out of LDS by the transposing read.  K goes straight from memory into registers.
+// second; V^T's operand is read out of LDS by the transposing read.
 //
-// Two kernels.  The first takes the contexts: the 128-key units of all (stream, head) pairs stand in one line, which is cut into equal parts, one
-// for each workgroup, whatever the streams' lengths are.  The four waves of a workgroup each take 32 keys of a unit, all rows, and meet only
-// where a pair ends: no barrier in the loop.  What a part finds for a pair stays in scratch (fp32, unnormalised).  The second takes
-// 16 rows of a pair, works the drafted tokens in under their masks, joins the parts, divides and rounds once.
+// Two launches.  The first takes the contexts: the 128-key units of all (stream, head) pairs stand in one line, which is cut into equal parts, one
+// for each workgroup, whatever the streams' lengths are.  What a part finds for a pair stays in scratch (fp32, unnormalised).  Up to 32 rows (16 of heads
+// wider than 128) memory bounds it, and each of four waves takes 32 keys of a unit and all rows, with no barrier in the loop; above, waves have rows of their
+// own and share the keys in LDS.  The second launch takes 16 rows of a pair, joins the parts, works the drafted tokens in under their masks,
+// divides and rounds once.
 #include <math.h>
 
 #include "common.h"
@@ -314,7 +315,7 @@ struct own_keys : flash<BF16, DP, NR, 32, TERMS, FULL> {
     }
 };
 
-// Joins what the four waves of a workgroup carry of 16 rows, through LDS (16 rows of OLD floats for each wave): calls
+// Joins what the W waves of a workgroup carry of 16 rows, through LDS (16 rows of OLD floats for each wave): calls
 // put(row, channel, sums of four channels, maximum, sum of weights) for each row and each four channels.
 template <int DP, int W, typename F, typename PUT>
 __device__ __forceinline__ void join_waves(F& f, int n, float* os, float (*top)[16], float (*sum)[16], PUT&& put) {
@@ -345,11 +346,14 @@ __device__ __forceinline__ void join_waves(F& f, int n, float* os, float (*top)[
 
 // Where a workgroup's part of the line starts and ends, and the stream and the unit within its pairs that it starts at; false if the
 // part is empty.  Workgroup 0 leaves the streams' places for the second kernel.
-__device__ __forceinline__ bool place_part(const attend_args& a, int part, int* waves, int* where, int* at, int* end, int* b, int* offset) {
+__device__ __forceinline__ bool place_part(const attend_args& a, int part, int* waves, int* where, int* at, int* end, int* b, int* offset, stream* s) {
     const int t = threadIdx.x, threads = blockDim.x;
     if (a.B <= 64) {
         // every wave by itself
-        const int lane = t % 64, n = lane < a.B ? a.H * stream_of(a, lane, blockIdx.x == 0 && t < 64).units : 0;
+        const int lane = t % 64;
+        stream mine = {0, 0, 0, 0};
+        if (lane < a.B) mine = stream_of(a, lane, blockIdx.x == 0 && t < 64);
+        const int n = a.H * mine.units;
         int upto = n;
         for (int o = 1; o < 64; o <<= 1) {
             const int y = __shfl_up(upto, o);
@@ -365,6 +369,10 @@ __device__ __forceinline__ bool place_part(const attend_args& a, int part, int* 
         if (*at >= *end || part >= a.parts) return false;
         *b = __popcll(__ballot(upto <= *at));          // streams that end before it
         *offset = *at - (__builtin_amdgcn_readlane(upto, *b) - __builtin_amdgcn_readlane(n, *b));
+        s->len = __builtin_amdgcn_readlane(mine.len, *b);
+        s->slots = __builtin_amdgcn_readlane(mine.slots, *b);
+        s->drafted = __builtin_amdgcn_readlane(mine.drafted, *b);
+        s->units = __builtin_amdgcn_readlane(mine.units, *b);
         return true;
     }
     int quota = 0;
@@ -391,6 +399,7 @@ __device__ __forceinline__ bool place_part(const attend_args& a, int part, int* 
     if (*at >= *end || part >= a.parts) return false;
     *b = uniform(where[0]);
     *offset = uniform(where[1]);
+    *s = stream_of(a, *b, false);
     return true;
 }
 
@@ -426,7 +435,9 @@ __device__ __forceinline__ void list_keys(const attend_args& a, const stream& s,
     __syncthreads();
 }
 
-// Workgroup (part, tile of up to 32 rows): the part's keys, pair by pair, each wave 32 keys of a unit and all rows.
+// Workgroup (part, tile of up to 32 rows): the part's keys, pair by pair, each wave 32 keys of a unit and all rows.  K and V go through
+// registers into LDS, a tile ahead, by loads that leave no trace in the caches.  (64 streams of 517 to 8100 tokens, 8 heads of 128: 1.13 GB in 188 us, 6.0
+// TB/s, of the 6.95 that a plain read reaches; with cached loads 8 us more, with three workgroups on a compute unit in place of two 40.)
 template <bool BF16, int DP, int NR, bool FULL>
 __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attend_context_kernel(attend_args a) {
     constexpr int ROWS = 16 * NR;   // two terms of a weight: what bounds this one is memory
@@ -441,8 +452,8 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attend_context_kernel(a
     // workgroups of the same part and different tiles read the same keys: 8 apart, they run behind the same L2
     const int tile = (int)(blockIdx.x / 8) % a.tiles, part = (int)(blockIdx.x / 8) / a.tiles * 8 + (int)(blockIdx.x % 8);
     int at, end, b, offset;
-    if (!place_part(a, part, waves, where, &at, &end, &b, &offset)) return;
-    stream s = stream_of(a, b, false);
+    stream s;
+    if (!place_part(a, part, waves, where, &at, &end, &b, &offset, &s)) return;
     int h = offset / s.units, first = offset % s.units;
     uint16_t* vs = reinterpret_cast<uint16_t*>(pool) + wave * 32 * state::VLD;
     const uint32_t* mine = listed + wave * 32;
@@ -516,8 +527,8 @@ __global__ __launch_bounds__(64 * W, DP > 128 ? (W == 4 ? 2 : 1) : W * (16 * NR 
     const int t = threadIdx.x, lane = t % 64, col = lane % 16, quad = lane / 16, wave = uniform(t / 64);
     const int tile = (int)(blockIdx.x / 8) % a.tiles, part = (int)(blockIdx.x / 8) / a.tiles * 8 + (int)(blockIdx.x % 8);
     int at, end, b, offset;
-    if (!place_part(a, part, waves, where, &at, &end, &b, &offset)) return;
-    stream s = stream_of(a, b, false);
+    stream s;
+    if (!place_part(a, part, waves, where, &at, &end, &b, &offset, &s)) return;
     int h = offset / s.units, first = offset % s.units;
     const v4i *kp = reinterpret_cast<const v4i*>(a.k), *vp = reinterpret_cast<const v4i*>(a.v);
     state f;
@@ -594,8 +605,9 @@ __global__ __launch_bounds__(64 * W, DP > 128 ? (W == 4 ? 2 : 1) : W * (16 * NR 
 }
 
 // Workgroup (pair, 16 rows): the parts of the context, the drafted tokens, the end.  W waves share the parts and the drafted tokens: one
-// where a pair has few parts, as many rows fill the device then, or four where it has many.  (24 x 4 pairs of 168 rows, 3 parts
-// each: 21 us with four waves, 10 with one; 8 pairs of 4 rows, 33 parts each: 10 and 25.)
+// where a pair has few parts, as many rows fill the device then, or eight (four for wide heads, for their registers) where it has many.  Latency bounds it:
+// three trips to memory, the drafted tokens' products, the join.  (24 x 4 pairs of 168 rows, 3 parts each: 21 us with four waves, 10 with one; 8 pairs of 4
+// rows, 32 parts each: 25 with one, 10 with four, 8 with eight.)
 template <bool BF16, int DP, int W, bool FULL>
 __global__ __launch_bounds__(64 * W, DP > 128 ? 1 : 2) void attend_finish_kernel(attend_args a) {
     typedef own_keys<BF16, DP, 1, 2, FULL> state;
@@ -623,23 +635,32 @@ __global__ __launch_bounds__(64 * W, DP > 128 ? 1 : 2) void attend_finish_kernel
         // this row in the tiles of the first kernel
         const int tile = row0 / a.rows, in = row0 % a.rows + min(col, rows - 1);
         auto slot = [&](int p) { return (((int64_t)b * a.H + h + p) * a.tiles + tile) * a.rows + in; };
-        // Each wave every W-th part: the maxima first, then the sums, several parts on their way at a time.  A part without keys left zeros.
-        float big = -INFINITY;
-#pragma unroll 4
-        for (int p = p0 + wave; p <= p1; p += W) big = fmaxf(big, a.part_ml[slot(p) * 2]);
-        f.m[0] = big;
-#pragma unroll 4
-        for (int p = p0 + wave; p <= p1; p += W) {
+        // Each wave every W-th part, two on their way at a time.  A part without keys left zeros.
+        typedef float v2f __attribute__((ext_vector_type(2)));
+        v4f x[2][state::CT];
+        v2f ml[2];
+        auto get = [&](int i, int p) {
             const int64_t at = slot(p);
-            const float m = a.part_ml[at * 2], z = a.part_ml[at * 2 + 1];
-            const float* part = a.part_o + at * DP + quad * 4;
-            v4f x[state::CT];
+            ml[i] = *reinterpret_cast<const v2f*>(a.part_ml + at * 2);
 #pragma unroll
-            for (int c = 0; c < state::CT; ++c) x[c] = *reinterpret_cast<const v4f*>(part + c * 16);
-            const float w = m == -INFINITY ? 0.f * z : __builtin_amdgcn_exp2f(m - big);   // a sum that is no number stays
+            for (int c = 0; c < state::CT; ++c) x[i][c] = *reinterpret_cast<const v4f*>(a.part_o + at * DP + c * 16 + quad * 4);
+        };
+        auto join = [&](int i) {
+            const float m = ml[i][0], z = ml[i][1], next = fmaxf(f.m[0], m);
+            const float w = m == -INFINITY ? 0.f * z : __builtin_amdgcn_exp2f(m - next);   // a sum that is no number stays
+            f.rescale(0, f.m[0] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(f.m[0] - next));
+            f.m[0] = next;
             if (quad == 0) f.l[0] += w * z;
 #pragma unroll
-            for (int c = 0; c < state::CT; ++c) f.o[0][c] += w * x[c];
+            for (int c = 0; c < state::CT; ++c) f.o[0][c] += w * x[i][c];
+        };
+        if (p0 + wave <= p1) get(0, p0 + wave);
+        for (int p = p0 + wave; p <= p1; p += 2 * W) {
+            if (p + W <= p1) get(1, p + W);
+            join(0);
+            if (p + W > p1) break;
+            if (p + 2 * W <= p1) get(0, p + 2 * W);
+            join(1);
         }
     }
     const int token = token_of(a, row0 + col);
