@@ -141,9 +141,10 @@ __device__ __forceinline__ int quota_of(const attend_args& a, int units) { retur
 //   TERMS: how many terms of the cache's type a weight enters its product with v as.  Two are a weight to 2^-15 and more, and cost half as
 //   many products again.  The first is cut, not rounded, and the second is what is left and 2^-23 of the weight: neither is negative,
 //   nor 0 where the other is not, so that a value that is infinite stays so.
-template <bool BF16, int DP, int NR, int KT, int TERMS, bool FULL>
+//   CS: into how many shares the channels of the result are cut, of which it has one: CT tiles of 16 channels.
+template <bool BF16, int DP, int NR, int KT, int TERMS, bool FULL, int CS = 1>
 struct flash {
-    static constexpr int KS = DP / 32, CT = DP / 16;
+    static constexpr int KS = DP / 32, CT = DP / 16 / CS;
     static constexpr int VLD = DP + 16;          // LDS row of V in elements: 32 bytes behind each, so that 16 rows' reads meet no bank twice
     v4i qf[NR][KS], pf[NR][TERMS][KT / 32];
     v4f o[NR][CT], sc[NR][KT / 16];
@@ -272,9 +273,9 @@ struct flash {
 
 // The same with the wave's own keys: K and V through registers into the wave's LDS, one after the other in the same place.  Whole rows
 // come from memory at a time (as the operand of the first product K would come in 64 bytes of 16 rows).
-template <bool BF16, int DP, int NR, int TERMS, bool FULL>
-struct own_keys : flash<BF16, DP, NR, 32, TERMS, FULL> {
-    typedef flash<BF16, DP, NR, 32, TERMS, FULL> base;
+template <bool BF16, int DP, int NR, int TERMS, bool FULL, int CS = 1>
+struct own_keys : flash<BF16, DP, NR, 32, TERMS, FULL, CS> {
+    typedef flash<BF16, DP, NR, 32, TERMS, FULL, CS> base;
     static constexpr int LPR = DP <= 64 ? 8 : DP <= 128 ? 16 : 32, RPI = 64 / LPR, VI = 32 / RPI;   // lanes on a row, rows at a time, pieces of a lane
     static constexpr int KLD = DP + 8, VLD = base::VLD;                // LDS rows in elements: 16 rows' pieces of 16 bytes meet no bank twice
     v4i kr[VI], vr[VI];
@@ -317,18 +318,18 @@ struct own_keys : flash<BF16, DP, NR, 32, TERMS, FULL> {
 
 // Joins what the W waves of a workgroup carry of 16 rows, through LDS (16 rows of OLD floats for each wave): calls
 // put(row, channel, sums of four channels, maximum, sum of weights) for each row and each four channels.
-template <int DP, int W, typename F, typename PUT>
+template <int W, typename F, typename PUT>
 __device__ __forceinline__ void join_waves(F& f, int n, float* os, float (*top)[16], float (*sum)[16], PUT&& put) {
-    constexpr int OLD = DP + 4;
+    constexpr int CT = F::CT, OLD = CT * 16 + 4;
     const int t = threadIdx.x, col = t % 16, quad = t % 64 / 16, wave = t / 64;
     __syncthreads();
     const float l = rows_sum(f.l[n]);
     if (quad == 0) top[wave][col] = f.m[n], sum[wave][col] = l;
 #pragma unroll
-    for (int c = 0; c < DP / 16; ++c) *reinterpret_cast<v4f*>(os + (wave * 16 + col) * OLD + c * 16 + quad * 4) = f.o[n][c];
+    for (int c = 0; c < CT; ++c) *reinterpret_cast<v4f*>(os + (wave * 16 + col) * OLD + c * 16 + quad * 4) = f.o[n][c];
     __syncthreads();
-    for (int x = t; x < 16 * (DP / 4); x += 64 * W) {
-        const int r = x / (DP / 4), c = x % (DP / 4) * 4;
+    for (int x = t; x < 16 * (CT * 4); x += 64 * W) {
+        const int r = x / (CT * 4), c = x % (CT * 4) * 4;
         float big = top[0][r];
 #pragma unroll
         for (int w = 1; w < W; ++w) big = fmaxf(big, top[w][r]);
@@ -490,7 +491,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attend_context_kernel(a
             const int64_t slot = (((int64_t)b * a.H + h + part) * a.tiles + tile) * ROWS;
 #pragma unroll
             for (int r = 0; r < NR; ++r)
-                join_waves<DP, 4>(f, r, reinterpret_cast<float*>(pool), top, sum, [&](int row, int c, v4f y, float big, float z) {
+                join_waves<4>(f, r, reinterpret_cast<float*>(pool), top, sum, [&](int row, int c, v4f y, float big, float z) {
                     if (r * 16 + row >= rows) return;
                     *reinterpret_cast<v4f*>(a.part_o + (slot + r * 16 + row) * DP + c) = y;
                     if (c == 0) a.part_ml[(slot + r * 16 + row) * 2] = big, a.part_ml[(slot + r * 16 + row) * 2 + 1] = z;
@@ -607,17 +608,19 @@ __global__ __launch_bounds__(64 * W, DP > 128 ? (W == 4 ? 2 : 1) : W * (16 * NR 
 // Workgroup (pair, 16 rows): the parts of the context, the drafted tokens, the end.  W waves share the parts and the drafted tokens: one
 // where a pair has few parts, as many rows fill the device then, or eight (four for wide heads, for their registers) where it has many.  Latency bounds it:
 // three trips to memory, the drafted tokens' products, the join.  (24 x 4 pairs of 168 rows, 3 parts each: 21 us with four waves, 10 with one; 8 pairs of 4
-// rows, 32 parts each: 25 with one, 10 with four, 8 with eight.)
-template <bool BF16, int DP, int W, bool FULL>
+// rows, 32 parts each: 25 with one, 10 with four, 8 with eight.)  Where that are few workgroups, two share the channels, each with all scores: 8 pairs of 64
+// rows and 131000 tokens 123 us in all, so 117, 4 rows and 4096 tokens 17.6 and 16.6; with more they only do the scores twice (8 pairs of 256 rows 188 and 192,
+// 96 pairs of 512 rows 226 and 302).
+template <bool BF16, int DP, int W, int CS, bool FULL>
 __global__ __launch_bounds__(64 * W, DP > 128 ? 1 : 2) void attend_finish_kernel(attend_args a) {
-    typedef own_keys<BF16, DP, 1, 2, FULL> state;
+    typedef own_keys<BF16, DP, 1, 2, FULL, CS> state;
     constexpr uint32_t EXP = BF16 ? 0x7f80u : 0x7c00u;
     __shared__ __align__(16) unsigned char pool[W * 32 * state::VLD * 2];
     __shared__ float top[W][16], sum[W][16];
     const int t = threadIdx.x, lane = t % 64, wave = uniform(t / 64), col = lane % 16, quad = lane / 16;
-    const int row0 = blockIdx.y * 16, h = blockIdx.x % a.H, b = blockIdx.x / a.H;
+    const int row0 = blockIdx.y * 16, h = blockIdx.x % a.H, b = blockIdx.x / a.H, c0 = CS > 1 ? blockIdx.z * state::CT * 16 : 0;   // the share's first channel
     const int units = a.starts[a.B], start = a.starts[b];
-    const stream s = stream_of(a, b, blockIdx.y == 0 && h == 0);
+    const stream s = stream_of(a, b, blockIdx.y == 0 && h == 0 && c0 == 0);
     const int rows = min(s.drafted * a.G - row0, 16);
     if (rows <= 0) return;
     uint16_t* vs = reinterpret_cast<uint16_t*>(pool) + wave * 32 * state::VLD;
@@ -643,7 +646,7 @@ __global__ __launch_bounds__(64 * W, DP > 128 ? 1 : 2) void attend_finish_kernel
             const int64_t at = slot(p);
             ml[i] = *reinterpret_cast<const v2f*>(a.part_ml + at * 2);
 #pragma unroll
-            for (int c = 0; c < state::CT; ++c) x[i][c] = *reinterpret_cast<const v4f*>(a.part_o + at * DP + c * 16 + quad * 4);
+            for (int c = 0; c < state::CT; ++c) x[i][c] = *reinterpret_cast<const v4f*>(a.part_o + at * DP + c0 + c * 16 + quad * 4);
         };
         auto join = [&](int i) {
             const float m = ml[i][0], z = ml[i][1], next = fmaxf(f.m[0], m);
@@ -693,7 +696,7 @@ __global__ __launch_bounds__(64 * W, DP > 128 ? 1 : 2) void attend_finish_kernel
         f.put_v(vs, there);
         const uint32_t sees = word & there;
         f.weigh(a.scale_log2, &sees, false);
-        f.add(vs);
+        f.add(vs + c0);
         if (odd) {
             // One drafted token at a time: its values that are not numbers alone in LDS, and only the rows that weigh it take the product.
 #pragma unroll 1
@@ -719,7 +722,7 @@ __global__ __launch_bounds__(64 * W, DP > 128 ? 1 : 2) void attend_finish_kernel
                 const bool takes = rows_max(any ? 1.f : 0.f) > 0.f;
 #pragma unroll
                 for (int c = 0; c < state::CT; ++c) {
-                    const v4f x = mfma<BF16>(f.get_v(vs, c), alone, v4f{0.f, 0.f, 0.f, 0.f});
+                    const v4f x = mfma<BF16>(f.get_v(vs + c0, c), alone, v4f{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
                     for (int r = 0; r < 4; ++r) f.o[0][c][r] += takes ? x[r] : 0.f;
                 }
@@ -737,15 +740,15 @@ __global__ __launch_bounds__(64 * W, DP > 128 ? 1 : 2) void attend_finish_kernel
         const int64_t to = (((int64_t)b * a.T + i) * a.H + h) * a.G + (row0 + row - i * a.G);
         const bool some = z > 0.f || z != z;
         const float g = some ? 1.f / z : 0.f;
-        if (FULL || c < a.d) *reinterpret_cast<v2i*>(a.out + to * a.d + c) = v2i{pack<BF16>(y[0] * g, y[1] * g), pack<BF16>(y[2] * g, y[3] * g)};
-        if (c == 0 && a.lse) a.lse[to] = some ? (m + log2f(z)) * 0.693147180559945309f : -INFINITY;
+        if (FULL || c0 + c < a.d) *reinterpret_cast<v2i*>(a.out + to * a.d + c0 + c) = v2i{pack<BF16>(y[0] * g, y[1] * g), pack<BF16>(y[2] * g, y[3] * g)};
+        if (c0 + c == 0 && a.lse) a.lse[to] = some ? (m + log2f(z)) * 0.693147180559945309f : -INFINITY;
     };
     if constexpr (W == 1) {
         const float z = rows_sum(f.l[0]);
 #pragma unroll
         for (int c = 0; c < state::CT; ++c) put(col, c * 16 + quad * 4, f.o[0][c], f.m[0], z);
     } else {
-        join_waves<DP, W>(f, 0, reinterpret_cast<float*>(pool), top, sum, put);
+        join_waves<W>(f, 0, reinterpret_cast<float*>(pool), top, sum, put);
     }
 }
 
@@ -766,9 +769,10 @@ void launch_attend(const attend_args& a, hipStream_t stream) {
         else hipLaunchKernelGGL((attend_wide_kernel<BF16, DP, 8, 1, FULL>), grid, dim3(512), 0, stream, a);
     }
     constexpr int MANY = DP > 128 ? 4 : 8;      // eight waves would leave wide heads too few registers
-    const dim3 rows((unsigned)(a.B * a.H), (unsigned)((a.T * a.G + 15) / 16));
-    if ((a.parts - 1) / 4 < a.B * a.H && a.T <= 64) hipLaunchKernelGGL((attend_finish_kernel<BF16, DP, 1, FULL>), rows, dim3(64), 0, stream, a);
-    else hipLaunchKernelGGL((attend_finish_kernel<BF16, DP, MANY, FULL>), rows, dim3(64 * MANY), 0, stream, a);
+    const unsigned pairs = (unsigned)(a.B * a.H), rows = (unsigned)((a.T * a.G + 15) / 16);
+    if ((a.parts - 1) / 4 < a.B * a.H && a.T <= 64) hipLaunchKernelGGL((attend_finish_kernel<BF16, DP, 1, 1, FULL>), dim3(pairs, rows), dim3(64), 0, stream, a);
+    else if ((int64_t)pairs * rows >= 128) hipLaunchKernelGGL((attend_finish_kernel<BF16, DP, MANY, 1, FULL>), dim3(pairs, rows), dim3(64 * MANY), 0, stream, a);
+    else hipLaunchKernelGGL((attend_finish_kernel<BF16, DP, MANY, 2, FULL>), dim3(pairs, rows, 2), dim3(64 * MANY), 0, stream, a);
 }
 
 template <bool BF16, int DP>
