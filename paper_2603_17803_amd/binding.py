@@ -662,8 +662,8 @@ class Swarm:
             lse = self.torch.empty((B, T, HG), dtype=self._f32, device=self.device)
         new = (B, T, H, d)
         rc = swarm_tree_attend(self.ctx, c, layer, at(q, shape, kind, "q"), at(k_new, new, kind, "k_new"), at(v_new, new, kind, "v_new"), B, T, HG // H,
-                                         at(n_new, (B,), i32, "n_new"), at(mask, (B, T, (T + 31) // 32), i32, "mask"), at(sel, (B, H, n), i32, "sel"), n, per,
-                                         d ** -0.5 if scale is None else scale, at(out, shape, kind, "out"), at(lse, (B, T, HG), self._f32, "lse"))
+                               at(n_new, (B,), i32, "n_new"), at(mask, (B, T, (T + 31) // 32), i32, "mask"), at(sel, (B, H, n), i32, "sel"), n, per,
+                               d ** -0.5 if scale is None else scale, at(out, shape, kind, "out"), at(lse, (B, T, HG), self._f32, "lse"))
         if rc:
             self._check("swarm_tree_attend", rc)
         return out, lse
@@ -698,7 +698,7 @@ class Swarm:
         kind, i32, at, new = cache[0].dtype, self._i32, self._at, (c.L, B, T, c.H, c.d)
         length = self.torch.empty_like(cache[3]) if out is None else out
         rc = swarm_cache_append(self.ctx, c, at(k_new, new, kind, "k_new"), at(v_new, new, kind, "v_new"), B, T, at(path, (B, n_max), i32, "path"), n_max,
-                                          at(n, (B,), i32, "n"), at(length, (c.rows,), i32, "length"))
+                                at(n, (B,), i32, "n"), at(length, (c.rows,), i32, "length"))
         if rc:
             self._check("swarm_cache_append", rc)
         return Cache(cache[0], cache[1], cache[2], length, cache[4])
@@ -739,9 +739,9 @@ class Swarm:
                 raise ValueError("hist must be [B][K][cap] and comes with step and hist_out")
             cap = hist.shape[2]
         rc = swarm_beam_select(self.ctx, at(logits, shape, dtype, "logits"), self._kinds[dtype], stride, at(scores, (B, K), f32, "scores"),
-                                         at(finished, (B, K), self.torch.uint8, "finished"), eos, B, K, stride if vocab is None else vocab, k, at(score, (B, k), f32, "score"),
-                                         at(parent, (B, k), i32, "parent"), at(token, (B, k), i32, "token"), at(hist, (B, K, cap), i32, "hist"), at(step, (1,), i32, "step"),
-                                         cap, at(hist_out, (B, k, cap), i32, "hist_out"))
+                               at(finished, (B, K), self.torch.uint8, "finished"), eos, B, K, stride if vocab is None else vocab, k, at(score, (B, k), f32, "score"),
+                               at(parent, (B, k), i32, "parent"), at(token, (B, k), i32, "token"), at(hist, (B, K, cap), i32, "hist"), at(step, (1,), i32, "step"),
+                               cap, at(hist_out, (B, k, cap), i32, "hist_out"))
         if rc:
             self._check("swarm_beam_select", rc)
         return out

@@ -559,3 +559,10 @@ def test_scale_that_fp32_does_not_hold_in_units_of_ln_2(sw):
     p.scale = 3e38
     with pytest.raises(b.SwarmError):
         p.run(sw)
+
+
+@pytest.mark.parametrize("T,G,H,n,d", [(4, 4, 1, 1100000, 8), (3, 2, 2, 700000, 16), (3, 9, 1, 1100000, 8), (33, 2, 1, 1100000, 8), (40, 4, 1, 600000, 8), (4, 4, 1, 600000, 136)])
+def test_more_keys_of_a_pair_than_a_part_lists_at_a_time(sw, T, G, H, n, d):
+    """Parts of more than 2048 keys, so that rows are looked up several times.  Few keys weigh nearly all, another set for each row."""
+    p = Problem(T * G, "bf16", 1, T, H, G, d, 256, [n - 77], loud=8.0)
+    p.check(sw)
