@@ -412,7 +412,8 @@ typedef struct {
  * Products and sums are fp32, the sum of weights that of the fp32 weights.  A weight enters its product with v as two terms of the cache's type
  * (15 bits and more, so that the result is rounded once, at the end) where T*G <= 32 (16 for d > 128), and for the drafted tokens always; a
  * weight of the context beyond that is rounded to the type (off by half a step, as the result is by its own rounding).  What a token does not
- * see never reaches its result, infinities and NaN included.
+ * see never reaches its result, infinities and NaN included; an infinite value that it sees makes the result infinite, or NaN where its weight is below what
+ * the type holds.
  *
  * layer        which of the cache's L layers.
  * q            device, [B][T][H*G][d] in the cache's type, 16-byte aligned.   B <= rows streams, T drafted tokens each (1..256; one

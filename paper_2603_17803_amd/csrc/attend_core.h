@@ -492,7 +492,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attend_context_kernel(a
 #pragma unroll
             for (int r = 0; r < NR; ++r)
                 join_waves<4>(f, r, reinterpret_cast<float*>(pool), top, sum, [&](int row, int c, v4f y, float big, float z) {
-                    if (r * 16 + row >= rows) return;
+                    if (r * 16 + row >= rows || (!FULL && c >= a.d)) return;
                     *reinterpret_cast<v4f*>(a.part_o + (slot + r * 16 + row) * DP + c) = y;
                     if (c == 0) a.part_ml[(slot + r * 16 + row) * 2] = big, a.part_ml[(slot + r * 16 + row) * 2 + 1] = z;
                 });
@@ -589,7 +589,8 @@ __global__ __launch_bounds__(64 * W, DP > 128 ? (W == 4 ? 2 : 1) : W * (16 * NR 
                 const float l = rows_sum(f.l[r]);
                 if (row < rows) {
 #pragma unroll
-                    for (int c = 0; c < state::CT; ++c) *reinterpret_cast<v4f*>(a.part_o + (slot + row) * DP + c * 16 + quad * 4) = f.o[r][c];
+                    for (int c = 0; c < state::CT; ++c)
+                        if (FULL || c * 16 < a.d) *reinterpret_cast<v4f*>(a.part_o + (slot + row) * DP + c * 16 + quad * 4) = f.o[r][c];
                     if (quad == 0) a.part_ml[(slot + row) * 2] = f.m[r], a.part_ml[(slot + row) * 2 + 1] = l;
                 }
             }
@@ -646,7 +647,7 @@ __global__ __launch_bounds__(64 * W, DP > 128 ? 1 : 2) void attend_finish_kernel
             const int64_t at = slot(p);
             ml[i] = *reinterpret_cast<const v2f*>(a.part_ml + at * 2);
 #pragma unroll
-            for (int c = 0; c < state::CT; ++c) x[i][c] = *reinterpret_cast<const v4f*>(a.part_o + at * DP + c0 + c * 16 + quad * 4);
+            for (int c = 0; c < state::CT; ++c) x[i][c] = FULL || c0 + c * 16 < a.d ? *reinterpret_cast<const v4f*>(a.part_o + at * DP + c0 + c * 16 + quad * 4) : v4f{0.f, 0.f, 0.f, 0.f};
         };
         auto join = [&](int i) {
             const float m = ml[i][0], z = ml[i][1], next = fmaxf(f.m[0], m);
