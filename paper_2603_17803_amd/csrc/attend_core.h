@@ -380,7 +380,10 @@ __device__ __forceinline__ bool place_part(const attend_args& a, int part, int* 
     for (int pass = a.B <= threads; pass < 2; ++pass) {
         int before = 0, all;
         for (int base = 0; base < a.B; base += threads) {
-            const int i = base + t, n = i < a.B ? a.H * stream_of(a, i, blockIdx.x == 0).units : 0;
+            const int i = base + t;
+            stream mine = {0, 0, 0, 0};
+            if (i < a.B) mine = stream_of(a, i, blockIdx.x == 0);
+            const int n = a.H * mine.units;
             const int start = before + block_before(n, waves, &all);
             before += all;
             if (pass == 0 || a.B <= threads) {
@@ -390,7 +393,7 @@ __device__ __forceinline__ bool place_part(const attend_args& a, int part, int* 
                 *end = min(*at + quota, units);
             }
             if (pass) {
-                if (start <= *at && *at < start + n) where[0] = i, where[1] = *at - start;
+                if (start <= *at && *at < start + n) where[0] = i, where[1] = *at - start, where[2] = mine.len, where[3] = mine.slots, where[4] = mine.drafted, where[5] = mine.units;
                 if (blockIdx.x == 0 && i < a.B) a.starts[i] = start;
             }
         }
@@ -400,7 +403,7 @@ __device__ __forceinline__ bool place_part(const attend_args& a, int part, int* 
     if (*at >= *end || part >= a.parts) return false;
     *b = uniform(where[0]);
     *offset = uniform(where[1]);
-    *s = stream_of(a, *b, false);
+    *s = {uniform(where[2]), uniform(where[3]), uniform(where[4]), uniform(where[5])};
     return true;
 }
 
@@ -446,7 +449,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attend_context_kernel(a
     __shared__ __align__(16) unsigned char pool[4 * 32 * state::VLD * 2];
     __shared__ uint32_t listed[LISTED], held[LISTED / 32];
     __shared__ float top[4][16], sum[4][16];
-    __shared__ int waves[4], where[2];
+    __shared__ int waves[4], where[6];
     static_assert(4 * 16 * (DP + 4) * 4 <= sizeof(pool), "the waves' parts of the result fit their rows of V");
 
     const int wave = uniform(threadIdx.x / 64);
@@ -502,8 +505,10 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attend_context_kernel(a
         first = 0;
         if (++h == a.H) {
             h = 0;
-            do s = stream_of(a, ++b, false);
-            while (s.units == 0);
+            do {
+                if (++b >= a.B) return;
+                s = stream_of(a, b, false);
+            } while (s.units == 0);
         }
     }
 }
@@ -523,7 +528,7 @@ __global__ __launch_bounds__(64 * W, DP > 128 ? (W == 4 ? 2 : 1) : W * (16 * NR 
     constexpr int LPR = DP / 8, PIECES = KT * LPR, MINE = (PIECES + THREADS - 1) / THREADS;
     __shared__ __align__(16) uint16_t ks[2][KT * KLD], vs[2][KT * VLD];
     __shared__ uint32_t listed[LISTED], held[LISTED / 32];
-    __shared__ int waves[W], where[2];
+    __shared__ int waves[W], where[6];
 
     const int t = threadIdx.x, lane = t % 64, col = lane % 16, quad = lane / 16, wave = uniform(t / 64);
     const int tile = (int)(blockIdx.x / 8) % a.tiles, part = (int)(blockIdx.x / 8) / a.tiles * 8 + (int)(blockIdx.x % 8);
@@ -600,8 +605,10 @@ __global__ __launch_bounds__(64 * W, DP > 128 ? (W == 4 ? 2 : 1) : W * (16 * NR 
         first = 0;
         if (++h == a.H) {
             h = 0;
-            do s = stream_of(a, ++b, false);
-            while (s.units == 0);
+            do {
+                if (++b >= a.B) return;
+                s = stream_of(a, b, false);
+            } while (s.units == 0);
         }
     }
 }
@@ -635,7 +642,7 @@ __global__ __launch_bounds__(64 * W, DP > 128 ? 1 : 2) void attend_finish_kernel
         f.load(f.vr, vp, a.d, row);
     }
     if (s.units > 0) {
-        const int g = start + h * s.units, quota = quota_of(a, units), p0 = g / quota, p1 = (g + s.units - 1) / quota;
+        const int g = start + h * s.units, quota = quota_of(a, units), p0 = g / quota, p1 = min((g + s.units - 1) / quota, a.parts - 1);
         // this row in the tiles of the first kernel
         const int tile = row0 / a.rows, in = row0 % a.rows + min(col, rows - 1);
         auto slot = [&](int p) { return (((int64_t)b * a.H + h + p) * a.tiles + tile) * a.rows + in; };
