@@ -7,7 +7,7 @@
 // with the second kernel, 5.0 TB/s), and with 16-bit logits the candidates: without the few that each chunk adds after the first, and the waits of
 // the other waves for the one that adds them, k = 16 takes 42 us in place of 54; the exponentials cost nothing.
 //
-// A second kernel, a workgroup for each group of beams, merges the sorted lists one candidate at a time and moves the histories.
+// A second kernel, a workgroup for each group of beams, merges the sorted lists and moves the histories.
 #include <math.h>
 
 #include <type_traits>
@@ -38,7 +38,7 @@ struct beam_args {
     double* refs;                                // [rows][J], in units of ln 2
     int32_t* found;                              // [rows][J]
     u64* lists;                                  // [rows][J][k]
-    int eos, K, V, k, hist_cap, J, per, trim;    // per: vectors of 16 bytes of a slice; trim: candidates from which a list is cut down
+    int eos, K, V, k, hist_cap, J, per, trim, halving;    // per: vectors of 16 bytes of a slice; trim: candidates from which a list is cut down
 };
 
 // Logits in their order as unsigned integers; 0 is below all of them.
@@ -327,14 +327,14 @@ __device__ __forceinline__ u64 ordered(double x) {
 }
 __device__ __forceinline__ double score_of(u64 key) { return __longlong_as_double((long long)(key >> 63 ? key & ~((u64)1 << 63) : ~key)); }
 
-// Workgroup b.  Its first wave merges: a lane has every 64th of the K * J lists and the best candidate among them, and each round takes
+// Workgroup b.  Few lists are merged by all threads at once; otherwise its first wave merges: a lane has every 64th of the K * J lists and the best candidate among them, and each round takes
 // the best lane's.  Then all move the histories.
 __global__ __launch_bounds__(1024) void beam_join_kernel(beam_args a) {
     __shared__ double norm[64];                  // ln sum exp of each beam's logits; of a finished one nothing
     __shared__ float base[64];
     __shared__ uint8_t head[MOST_LISTS], length[MOST_LISTS], beams[MOST_LISTS];   // where each list stands, its candidates (255: the one of a finished beam), its beam
     __shared__ u64 staged[STAGED], scored[STAGED];   // candidates, and their scores
-    __shared__ int parent[128], token[128];
+    __shared__ int parent[128], token[128], places[STAGED];
     __shared__ float best[128];
     const int64_t b = blockIdx.x;
     const int t = threadIdx.x, lists = a.K * a.J, n_staged = lists * a.k <= STAGED ? lists * a.k : 0;
@@ -370,10 +370,50 @@ __global__ __launch_bounds__(1024) void beam_join_kernel(beam_args a) {
     };
     for (int i = t; i < n_staged; i += 1024) {
         const int list = i / a.k;
-        if (i - list * a.k < length[list] && length[list] != 255) scored[i] = score_of_key(beams[list], staged[i], false);
+        const bool finished = length[list] == 255;
+        if (finished && i == list * a.k) staged[i] = candidate(0.f, a.eos);
+        if (i - list * a.k < (finished ? 1 : length[list])) scored[i] = score_of_key(beams[list], staged[i], finished);
+    }
+    const bool searched = n_staged && a.k >= 4 && lists <= 24;
+    if (searched) {
+        for (int i = t; i < n_staged; i += 1024) places[i] = i % a.k;
+        if (t < a.k) parent[t] = -1, token[t] = -1, best[t] = -INFINITY;
     }
     __syncthreads();
-    if (t < 64) {
+    if (searched) {
+        // A candidate's place is how many stand above it: in each list the first few, found by halving.  The lists are divided over as many threads
+        // as there are for a candidate.  Its work grows with the square of the lists, that of the rounds below with k: 64 groups of 16 lists take 54 us
+        // by rounds and 52 so for k = 16, 89 and 83 for k = 64, 130 and 120 for k = 128 (the whole call); 8 groups of 124 lists, k = 8, 21 and 127.
+        const int shares = max(1, 1024 / n_staged);
+        for (int x = t; x < n_staged * shares; x += 1024) {
+            const int share = x / n_staged, i = x - share * n_staged, list = i / a.k, beam = beams[list];
+            if (i - list * a.k >= (length[list] == 255 ? 1 : length[list])) continue;
+            const u64 score = scored[i], key = staged[i];
+            int above = 0;
+            for (int l = share; l < lists; l += shares) {
+                const int n = l == list ? 0 : length[l] == 255 ? 1 : length[l], other = beams[l], from = l * a.k;
+                int first = 0;
+                for (int step = a.halving; step; step >>= 1) {
+                    const int at = first + step - 1;
+                    if (at < n) {
+                        const u64 s = scored[from + at];
+                        first += s > score || (s == score && (other < beam || (other == beam && staged[from + at] > key))) ? step : 0;
+                    }
+                }
+                above += first;
+            }
+            if (above) atomicAdd(&places[i], above);
+        }
+        __syncthreads();
+        for (int i = t; i < n_staged; i += 1024) {
+            const int list = i / a.k, place = places[i];
+            if (i - list * a.k < (length[list] == 255 ? 1 : length[list]) && place < a.k) {
+                parent[place] = (int)(b * a.K) + beams[list];
+                token[place] = token_of(staged[i]);
+                best[place] = (float)score_of(scored[i]);
+            }
+        }
+    } else if (t < 64) {
         // The lane's best candidate (score 0: none), its beam and its list; where it has one list alone, the candidate behind it too.
         u64 score = 0, key = 0, behind = 0, behind_score = 0;
         int owner = 0, mine = t, at = 0, n = 0;
@@ -525,6 +565,7 @@ extern "C" swarm_status swarm_beam_select(swarm_ctx* ctx, const void* logits, in
     a.found = reinterpret_cast<int32_t*>(a.refs + slices);
     a.eos = eos, a.K = K, a.V = V, a.k = k, a.hist_cap = hist_cap, a.J = (int)J, a.per = (int)((vectors + J - 1) / J);
     // Cutting a list costs barriers and gives a higher bound: 512 rows of 128001 bf16 logits, k = 16 (32): at 48 (96) candidates 54 us (66), at 64 (128) 55 (69).
+    for (a.halving = 1; a.halving * 2 <= k;) a.halving *= 2;
     a.trim = 3 * k < 48 ? 48 : 3 * k;            // below 512
     if (dtype == SWARM_FP32) launch_beams<SWARM_FP32>(a, (int64_t)rows, ctx->stream);
     else if (dtype == SWARM_BF16) launch_beams<SWARM_BF16>(a, (int64_t)rows, ctx->stream);

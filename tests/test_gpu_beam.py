@@ -307,3 +307,19 @@ def test_fewer_beams_are_recorded_after_more(sw):
                 [x.zero_() for x in out]
             b.swarm_graph_destroy(graph)
         s.close()
+
+
+@pytest.mark.parametrize("K,V", [(24, 300), (25, 300), (3, 30000), (6, 14000), (7, 14000), (1, 60000), (64, 100)])
+@pytest.mark.parametrize("k", [3, 4, 7, 33, 128])
+def test_lists_merged_at_once_and_in_rounds(sw, K, V, k):
+    """Either side of the sizes that merge at once: plain, beams alike, some finished, some without a finite logit, NaN scores."""
+    logits, scores = random(K + k, 2, K, V, "fp32")
+    check(sw, logits, scores, k)
+    same = logits[:, :1].expand(2, K, V).contiguous()
+    check(sw, same, torch.zeros_like(scores), k)
+    check(sw, torch.zeros_like(logits), torch.zeros_like(scores), k)
+    done = (torch.arange(2 * K).reshape(2, K) % 3 == 1).to(torch.uint8)
+    scores[0, 0], scores[1, K // 2] = math.nan, -math.inf
+    logits[0, K - 1] = -math.inf
+    logits[1, K - 1, 5:] = -math.inf
+    check(sw, logits, scores, k, done, eos=17)
