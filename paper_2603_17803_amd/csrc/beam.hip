@@ -214,11 +214,12 @@ __global__ __launch_bounds__(256) void beam_slice_kernel(beam_args a) {
     bool every = bound == -INFINITY;
     float floor = every ? -INFINITY : below(bound);
     // Exponentials refer to the first chunk's largest logit, as 2^(x log2 e - at); a thread that meets a logit far above it refers to that one
-    // from then on.  `at` is rounded, and stands for the logit at / log2 e exactly.
-    constexpr float LOG2E = 1.44269504088896341f;
+    // from then on.  `at` is rounded, and stands for the logit at / log2 e exactly.  log2 e is taken in two parts, as what fp32 leaves out of it (2^-26 of
+    // it) grows with the logits and not with their differences: logits of 300 would be off by 4e-6 all the same way.
+    constexpr float LOG2E = 1.44269504088896341f, LOG2E_REST = (float)(1.4426950408889634074 - (double)LOG2E);
     float at2 = high == -INFINITY ? 0.f : high * LOG2E;
     double total = 0.0;
-    auto weight = [&](float x, float to) { return __builtin_amdgcn_exp2f(__builtin_fmaf(x, LOG2E, -to)); };
+    auto weight = [&](float x, float to) { return __builtin_amdgcn_exp2f(__builtin_fmaf(x, LOG2E_REST, __builtin_fmaf(x, LOG2E, -to))); };
     auto take = [&](const v4i (&v)[VECS], int chunk) {
         if (chunk > from) {
             __syncthreads();
