@@ -489,8 +489,8 @@ swarm_status swarm_cache_compact(swarm_ctx* ctx, const swarm_cache* cache, int32
 /*
  * Beam search's selection.  Each of B groups has K beams with running scores; a beam's candidates are the V tokens:
  *     score(beam, token) = scores[b][beam] + x - ln sum_t exp(x_t),   x = logits[b][beam][token]
- * in 64 bits from exponentials of 32 (the logarithm is good to about 1e-7), rounded to fp32 once, at the end.  A NaN logit counts as -inf, and
- * so does a score that comes out as NaN.  A finished beam has one candidate, token eos with the beam's score as it is.
+ * in 64 bits from exponentials of 32, rounded to fp32 once, at the end.  The logarithm is good to about 1e-7 whatever the logits' level and order (to 3e-6 where
+ * equal logits far below the largest make up the sum, whose roundings then all point one way).  A NaN logit counts as -inf, and so does a score that comes out as NaN.  A finished beam has one candidate, token eos with the beam's score as it is.
  * The k best candidates of a group come out in descending score; equal scores are won by the lower beam, and within a
  * beam by the higher logit, then by the lower token.  Where a group has fewer than k candidates, the rest is parent = token = -1 and score = -inf.
  *

@@ -213,11 +213,15 @@ __global__ __launch_bounds__(256) void beam_slice_kernel(beam_args a) {
     // the lower tokens.
     bool every = bound == -INFINITY;
     float floor = every ? -INFINITY : below(bound);
-    // Exponentials refer to the first chunk's largest logit, as 2^(x log2 e - at); a thread that meets a logit far above it refers to that one
-    // from then on.  `at` is rounded, and stands for the logit at / log2 e exactly.  log2 e is taken in two parts, as what fp32 leaves out of it (2^-26 of
+    // Exponentials refer to the first chunk's largest logit, as 2^(x log2 e - at); a thread that meets a logit more than 8 octaves above it, candidate or
+    // not, refers to that one from then on, so that no exponential overflows or has an argument that rounds far off.  Where the first chunk has no finite
+    // logit, a thread's first one is its reference.  `at` is rounded, and stands for the logit at / log2 e exactly.  log2 e is taken in two parts, as what fp32 leaves out of it (2^-26 of
     // it) grows with the logits and not with their differences: logits of 300 would be off by 4e-6 all the same way.
     constexpr float LOG2E = 1.44269504088896341f, LOG2E_REST = (float)(1.4426950408889634074 - (double)LOG2E);
-    float at2 = high == -INFINITY ? 0.f : high * LOG2E;
+    constexpr float ABOVE = 5.5f;                // just below 8 octaves
+    float at2 = high == -INFINITY ? -3.4e38f : high * LOG2E;
+    float edge = high + ABOVE;                   // from which logit on the reference is raised; -inf: there is none yet
+    float gate = fminf(floor, edge);
     double total = 0.0;
     auto weight = [&](float x, float to) { return __builtin_amdgcn_exp2f(__builtin_fmaf(x, LOG2E_REST, __builtin_fmaf(x, LOG2E, -to))); };
     auto take = [&](const v4i (&v)[VECS], int chunk) {
@@ -231,6 +235,7 @@ __global__ __launch_bounds__(256) void beam_slice_kernel(beam_args a) {
                 trim(list, n, a.k, best, &count);
                 floor = logit_of(list[a.k - 1]);
             }
+            gate = fminf(floor, edge);
         }
         const bool plain = whole(chunk);
 #pragma unroll
@@ -244,10 +249,12 @@ __global__ __launch_bounds__(256) void beam_slice_kernel(beam_args a) {
             }
 #pragma unroll
             for (int e = 0; e < E; e += 2) top = fmaxf(fmaxf(top, x[e]), x[e + 1]);
-            if (top > floor || every) {
-                if (top * LOG2E > at2 + 80.f) {
+            if (top > gate || every) {
+                if (top > edge) {
                     total *= exp2((double)at2 - (double)(top * LOG2E));
                     at2 = top * LOG2E;
+                    edge = top + ABOVE;
+                    gate = fminf(floor, edge);
                 }
                 uint32_t m = 0;
 #pragma unroll
@@ -279,7 +286,8 @@ __global__ __launch_bounds__(256) void beam_slice_kernel(beam_args a) {
     const int n = trim(list, pushed, a.k, best, &count);
     for (int i = t; i < n; i += 256) a.lists[at * a.k + i] = list[i];
     double big;
-    if (__syncthreads_or(total != total || !(fabsf(at2) < 1e5f))) {
+    const bool met = edge > -INFINITY;           // a finite logit, or one in the workgroup's first chunk
+    if (__syncthreads_or(!(total < INFINITY) || (met && !(fabsf(at2) < 1e5f)))) {
         // A logit that is no number or infinite, or logits so large that 2^(x log2 e - at) says nothing: the sum again, in 64 bits, referred to the
         // best candidate.  (A candidate of +inf leaves no number, as the definition does.)
         const double best_logit = n ? logit_of(list[0]) : -INFINITY;
@@ -298,7 +306,7 @@ __global__ __launch_bounds__(256) void beam_slice_kernel(beam_args a) {
     } else {
         // The threads' sums at one reference.  Added in 64 bits, they are off by the rounding of the largest exponentials above all: those of the list
         // are taken again in 64 bits in place of the 32 (unless references differ, where 1e-7 is what the logarithm is good to).
-        float high2 = at2, small = at2;
+        float high2 = at2, small = met ? at2 : 3.4e38f;
         for (int o = 32; o; o >>= 1) high2 = fmaxf(high2, __shfl_xor(high2, o)), small = fminf(small, __shfl_xor(small, o));
         if (lane == 0) ref[t / 64] = high2, low[t / 64] = small;
         __syncthreads();

@@ -74,11 +74,60 @@ def noise(seed, B, K, V, spread=3.0):
     return torch.randn((B, K, V), generator=g) * spread, torch.randn((B, K), generator=g) * 2 - 20
 
 
+def leads(B, K, V):
+    """Where a slice's first step stands, and a little behind it."""
+    rows = B * K
+    J = min(-(-1024 // rows), -(-(V + 8) // 4096), 64)
+    at = torch.arange(V)
+    return at % -(-V // J) < 4200
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("B,K,V,k", SIZES)
 def test_plain(sw, dtype, B, K, V, k):
     logits, scores = noise(1, B, K, V)
     check(sw, logits.to(TYPES[dtype]), scores, k)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("B,K,V,k", SIZES)
+def test_first_tokens_banned(sw, dtype, B, K, V, k):
+    """Each slice starts with banned tokens; of the others some are allowed, far above."""
+    logits, scores = noise(2, B, K, V)
+    allowed = torch.rand(V, generator=torch.Generator().manual_seed(3)) < 0.02
+    logits[..., leads(B, K, V) | ~allowed] = -100.0
+    check(sw, logits.to(TYPES[dtype]), scores, k)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rising_in_steps(sw, dtype):
+    """Very low ones, a few high ones, then many between: these are no candidates, and far above what came first."""
+    B, K, V, k = SIZES[0]
+    logits, scores = noise(4, B, K, V, 0.5)
+    logits += 5.0
+    for low in (-1e4, -60000.0):
+        for at in (0, -(-V // 2)):                                                         # the two slices of a row
+            logits[..., at:at + 8200] = low
+            logits[..., at + 5000:at + 5100] = 10.0 + 0.01 * torch.arange(100)
+        check(sw, logits.to(TYPES[dtype]), scores, k)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("level", [-30.0, -100.0, -500.0, -1000.0, 200.0])
+@pytest.mark.parametrize("size", [0, 2])
+def test_first_tokens_masked_and_the_others_low(sw, dtype, level, size):
+    """Nothing finite in a slice's first step, and what follows far from 0."""
+    B, K, V, k = SIZES[size]
+    logits, scores = noise(5, B, K, V, 1.0)
+    logits += level
+    logits[..., leads(B, K, V)] = -math.inf
+    check(sw, logits.to(TYPES[dtype]), scores, k)
+    # few tokens at all, in some slices none
+    few = torch.rand(V, generator=torch.Generator().manual_seed(6)) < 2e-4
+    few[-3:] = True
+    logits[..., ~few] = -math.inf
+    logits[..., :] = torch.where(few, torch.where(logits.isinf(), level, logits), logits)
+    check(sw, logits.to(TYPES[dtype]), scores, 2)
 
 
 @pytest.mark.parametrize("shift", [300.0, -3000.0, 30000.0])
@@ -107,3 +156,28 @@ def test_many_equal_logits_below_one(sw, dtype):
         logits = torch.full((B, K, V), 12.3 - gap)
         logits[..., 15000], logits[..., 17] = 12.3, 12.2 - gap
         check(sw, logits.to(TYPES[dtype]), noise(9, B, K, 1)[1], k)
+
+
+@pytest.mark.parametrize("size", [0, 2])
+def test_values_that_are_not_numbers(sw, size):
+    B, K, V, k = SIZES[size]
+    logits, scores = noise(10, B, K, V)
+    flat = logits.view(B * K, V)
+    lead = leads(B, K, V)
+    at = int(torch.nonzero(~lead)[100])
+    flat[0, at] = math.nan
+    flat[1, at] = math.inf
+    check(sw, logits, scores, k)
+    flat[0, lead], flat[1] = -math.inf, -math.inf
+    check(sw, logits, scores, k)
+    if B * K > 16:
+        flat[2, at], flat[3, at] = 3e38, 1e30
+        flat[4, lead], flat[5, lead], flat[6, lead] = -1e30, -3e38, 1e6
+        flat[7], flat[8], flat[9] = 3e38, -3e38, -torch.finfo(torch.float32).max
+        flat[10, ~lead] = math.nan
+        flat[11, lead], flat[11, ~lead] = -math.inf, -3e38
+        flat[12, lead], flat[12, ~lead] = -math.inf, -2.3e38
+        flat[13, lead], flat[13, at] = -math.inf, math.inf
+        scores[2] = math.inf
+        scores[3, 1] = math.nan
+        check(sw, logits, scores, k)
