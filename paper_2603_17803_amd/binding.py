@@ -608,12 +608,16 @@ class Swarm:
     # anything made on the way, and the outputs that a call makes itself are not checked.
 
     def _at(self, t, shape, dtype, name: str):
-        """Address of a tensor of a given shape and type on the context's device; None stays None."""
+        """Address of a tensor of a given shape and type on the context's device; None stays None, and a tensor without elements, whose address
+        is NULL too, is refused."""
         if t is None:
             return None
         if t.shape != shape or t.dtype is not dtype or t.get_device() != self._index or not t.is_contiguous():
             raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {self.device}, not {t.dtype} {tuple(t.shape)} on {t.device}")
-        return t.data_ptr()
+        at = t.data_ptr()
+        if not at:
+            raise ValueError(f"{name} has no elements: its shape is {tuple(t.shape)}")
+        return at
 
     def _cache(self, cache: Cache, refs: bool) -> swarm_cache:
         """The C form of a cache after the checks of its tensors; `refs`: the call reads the counts."""
@@ -635,7 +639,7 @@ class Swarm:
                     scale: Optional[float] = None, out=None, lse=None, want_lse: bool = False):
         """Attention of T drafted tokens (T = 1: one decoded token) of each stream over its row of the cache, or over the selected pages or
         tokens of it, and over the drafted tokens that they see.  q [B][T][H*G][d] and k_new, v_new [B][T][H][d] in the cache's
-        type; n_new int32 [B]; mask int32 [B][T][ceil(T/32)] words (None: a chain); sel int32 [B][H][n] positions as score_select gives them, of
+        type; n_new int32 [B]; mask int32 [B][T][ceil(T/32)] words (None: a chain); sel int32 [B][H][n >= 1] positions as score_select gives them, of
         pages (unit 'page') or tokens ('token'); scale: d ** -0.5 unless given.  Returns (out [B][T][H*G][d], lse fp32 [B][T][H*G] or None)."""
         c = self._cache(cache, False)
         shape = q.shape
@@ -687,7 +691,7 @@ class Swarm:
 
     def cache_append(self, cache: Cache, k_new, v_new, n=None, path=None, out=None) -> Cache:
         """Puts n[b] tokens of each stream (all without n) behind what row b holds, in every layer: token path[b][i], or i without a path.
-        k_new, v_new [L][B][T][H][d] in the cache's type; n int32 [B]; path int32 [B][n_max].  Returns the cache with its new lengths;
+        k_new, v_new [L][B][T][H][d] in the cache's type; n int32 [B]; path int32 [B][n_max >= 1].  Returns the cache with its new lengths;
         `out` = length reuses the caller's tensor (not that of `cache`)."""
         c = self._cache(cache, False)
         shape = k_new.shape
