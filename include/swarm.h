@@ -411,7 +411,8 @@ typedef struct {
  * in later (from an SSD) are attended over in a call of their own, and the two results weighted by exp(lse - joint lse).
  * Products and sums are fp32, the sum of weights that of the fp32 weights.  A weight enters its product with v as two terms of the cache's type
  * (15 bits and more, so that the result is rounded once, at the end) where T*G <= 32 (16 for d > 128), and for the drafted tokens always; a
- * weight of the context beyond that is rounded to the type (off by half a step, as the result is by its own rounding).  What a token does not
+ * weight of the context beyond that is rounded to the type (off by half a step, as the result is by its own rounding).  fp16 has no numbers for the smallest
+ * weights: there one is off by up to 2^-35 of the largest in any case. What a token does not
  * see never reaches its result, infinities and NaN included; an infinite value that it sees makes the result infinite, or NaN where its weight is below what
  * the type holds.
  *

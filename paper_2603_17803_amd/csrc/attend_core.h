@@ -23,7 +23,7 @@ struct attend_args {
     float* lse;
     int32_t* starts;                             // [B + 1]: where each stream's units start in the line, and their number
     float* part_o;                               // [slots][rows of a tile][DP]: sums of weighted values
-    float* part_ml;                              // [slots][rows of a tile][2]: maximum (in units of ln 2) and sum of weights
+    float* part_ml;                              // [slots][rows of a tile][2]: what weights refer to (in units of ln 2) and their sum
     uint32_t* flags;
     int P, H, page_log2, d, cap, B, T, G, n_sel, unit;
     int parts, tiles, rows;                      // parts of the line; tiles of a pair's rows, rows of a tile
@@ -146,6 +146,10 @@ template <bool BF16, int DP, int NR, int KT, int TERMS, bool FULL, int CS = 1>
 struct flash {
     static constexpr int KS = DP / 32, CT = DP / 16 / CS;
     static constexpr int VLD = DP + 16;          // LDS row of V in elements: 32 bytes behind each, so that 16 rows' reads meet no bank twice
+    // A row's weights are 2^(s - m).  m is raised to the row's maximum less LIFT when that has outgrown it by LAG more, so the largest weight is 2^LIFT to
+    // 2^(LIFT + LAG).  fp16 holds no number from 2^16 on and none below 2^-24, and bits fewer than all below 2^-14: its weights stand as high as they may,
+    // so that one is lost only below 2^-35 of the largest.  (At a maximum of 1 to 2^8, 131071 keys 25 octaves below one brought nothing.)
+    static constexpr float LAG = BF16 ? 8.f : 4.f, LIFT = BF16 ? 0.f : 11.f;
     v4i qf[NR][KS], pf[NR][TERMS][KT / 32];
     v4f o[NR][CT], sc[NR][KT / 16];
     float m[NR], l[NR];
@@ -192,9 +196,8 @@ struct flash {
         const v2i y = __builtin_bit_cast(v2i, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(from + 16 * VLD)));
         return v4i{x[0], x[1], y[0], y[1]};
     }
-    // The weights of KT keys; sees[j]: which of the keys 32 j to 32 j + 31 the lane's rows see.  The maximum that weights refer to is raised only
-    // when one of the 16 rows has outgrown it by 2^8: a row's weights stay below that, which no sum here minds, and most
-    // tiles rescale nothing.
+    // The weights of KT keys; sees[j]: which of the keys 32 j to 32 j + 31 the lane's rows see.  What weights refer to is raised only
+    // when one of the 16 rows has outgrown it: no sum here minds the larger weights, and most tiles rescale nothing.
     __device__ __forceinline__ void weigh(float scale_log2, const uint32_t* sees, bool all) {
         const int quad = threadIdx.x % 64 / 16;
         float mx[NR];
@@ -216,8 +219,8 @@ struct flash {
             mx[n] = -INFINITY;
 #pragma unroll
             for (int e = 0; e < KT / 16; ++e) mx[n] = fmaxf(fmaxf(fmaxf(mx[n], sc[n][e][0]), fmaxf(sc[n][e][1], sc[n][e][2])), sc[n][e][3]);
-            mx[n] = rows_max(mx[n]);
-            grown |= mx[n] > m[n] + 8.f;
+            mx[n] = rows_max(mx[n]) - LIFT;
+            grown |= mx[n] > m[n] + LAG;
         }
         if (__any(grown)) {
 #pragma unroll
@@ -317,7 +320,7 @@ struct own_keys : flash<BF16, DP, NR, 32, TERMS, FULL, CS> {
 };
 
 // Joins what the W waves of a workgroup carry of 16 rows, through LDS (16 rows of OLD floats for each wave): calls
-// put(row, channel, sums of four channels, maximum, sum of weights) for each row and each four channels.
+// put(row, channel, sums of four channels, what weights refer to, sum of weights) for each row and each four channels.
 template <int W, typename F, typename PUT>
 __device__ __forceinline__ void join_waves(F& f, int n, float* os, float (*top)[16], float (*sum)[16], PUT&& put) {
     constexpr int CT = F::CT, OLD = CT * 16 + 4;
