@@ -53,6 +53,10 @@ class Cache(NamedTuple):
     refs: Any = None
 
 
+def _no_elements(t, name: str):
+    raise ValueError(f"{name} has no elements: its shape is {tuple(t.shape)}")
+
+
 class SwarmError(RuntimeError):
     def __init__(self, fn: str, code: int, text: str = ""):
         super().__init__(f"{fn} -> {code}: {text}")
@@ -614,10 +618,7 @@ class Swarm:
             return None
         if t.shape != shape or t.dtype is not dtype or t.get_device() != self._index or not t.is_contiguous():
             raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {self.device}, not {t.dtype} {tuple(t.shape)} on {t.device}")
-        at = t.data_ptr()
-        if not at:
-            raise ValueError(f"{name} has no elements: its shape is {tuple(t.shape)}")
-        return at
+        return t.data_ptr() or _no_elements(t, name)
 
     def _cache(self, cache: Cache, refs: bool) -> swarm_cache:
         """The C form of a cache after the checks of its tensors; `refs`: the call reads the counts."""
