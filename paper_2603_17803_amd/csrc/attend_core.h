@@ -751,6 +751,7 @@ __global__ __launch_bounds__(64 * W, DP > 128 ? 1 : 2) void attend_finish_kernel
         const int64_t to = (((int64_t)b * a.T + i) * a.H + h) * a.G + (row0 + row - i * a.G);
         const bool some = z > 0.f || z != z;
         const float g = some ? 1.f / z : 0.f;
+        if (!some) y = v4f{0.f, 0.f, 0.f, 0.f};       // scores of -inf alone, whatever the values were
         if (FULL || c0 + c < a.d) *reinterpret_cast<v2i*>(a.out + to * a.d + c0 + c) = v2i{pack<BF16>(y[0] * g, y[1] * g), pack<BF16>(y[2] * g, y[3] * g)};
         if (c0 + c == 0 && a.lse) a.lse[to] = some ? (m + log2f(z)) * 0.693147180559945309f : -INFINITY;
     };

@@ -1,5 +1,5 @@
-"""Attention over a paged cache where small weights decide: every stream's row holds the same pages, so that one part of the work is a whole long
-context."""
+"""Attention over a paged cache where small weights decide, and where nothing is weighed: every stream's row holds the same pages, so that one part of
+the work is a whole long context."""
 import math
 
 import pytest
@@ -78,3 +78,27 @@ def test_one_key_far_above_many(sw, dtype, d, T, G, gap, spread):
         bad = (out[b, i, h].double() - want).abs() / tol
         assert (bad <= 1).all(), f"off by {bad.max():.3g} tolerances, {((out[b, i, h].double() - want).abs() / want.abs()).max():.3g} of the value"
         assert abs(float(lse[b, i, h]) - (s.max() + p.sum().log()).item()) <= e + (n / 4 + 64) * 2.0 ** -24 + 2.0 ** -22 * (1 + gap)
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("T,G,d", [(1, 4, 64), (10, 8, 64), (3, 2, 256), (20, 4, 256)])
+@pytest.mark.parametrize("where", ["context", "drafted", "both"])
+def test_scores_of_minus_infinity_alone(sw, dtype, T, G, d, where):
+    """What a token sees may all score -inf, values infinite or not: 0, and -inf for lse."""
+    t, B = TYPES[dtype], 3
+    low = torch.zeros((40, d), dtype=t)
+    low[:, 0] = -math.inf
+    v = torch.ones((40, d), dtype=t)
+    v[7, 2], v[33, 5] = math.inf, math.nan
+    cache = shared_rows(low, v, B)
+    if where == "drafted":
+        cache = cache._replace(length=torch.zeros_like(cache.length))
+    q = torch.zeros((B, T, G, d), dtype=t)
+    q[..., 0] = 1.0
+    more = {}
+    if where != "context":
+        k_new, v_new = torch.zeros((B, T, 1, d), dtype=t), torch.ones((B, T, 1, d), dtype=t)
+        k_new[..., 0], v_new[:, 0, 0, 2] = -math.inf, math.inf
+        more = dict(k_new=k_new.cuda(), v_new=v_new.cuda())
+    out, lse = attend(sw, cache, q, **more)
+    assert (lse == -math.inf).all() and (out == 0).all()
