@@ -139,8 +139,9 @@ __device__ __forceinline__ int quota_of(const attend_args& a, int units) { retur
 // What a wave carries of NR * 16 query rows: lane l has row l % 16 of each 16, and of the sums of values the channels
 // 16 c + 4 (l / 16) + 0..3.  KT keys are taken at a time.
 //   TERMS: how many terms of the cache's type a weight enters its product with v as.  Two are a weight to 2^-15 and more, and cost half as
-//   many products again.  The first is cut, not rounded, and the second is what is left and 2^-23 of the weight: neither is negative,
-//   nor 0 where the other is not, so that a value that is infinite stays so.
+//   many products again.  The first is cut, not rounded, and the second is what is left and 2^-23 of the weight (in fp16, which has no such small numbers,
+//   its smallest number where nothing is left): neither is negative, and the second is not 0 where the first is not, so that a value that is
+//   infinite stays so.
 //   CS: into how many shares the channels of the result are cut, of which it has one: CT tiles of 16 channels.
 template <bool BF16, int DP, int NR, int KT, int TERMS, bool FULL, int CS = 1>
 struct flash {
@@ -186,6 +187,12 @@ struct flash {
                 for (int n = 0; n < NR; ++n) sc[n][k] = mfma<BF16>(kf, qf[n][c], sc[n][k]);
             }
         }
+    }
+    // What the first term leaves of a weight.  The middle one of three numbers is what is left or fp16's smallest number, where the weight is not below
+    // that, and the weight itself where it is.
+    static __device__ __forceinline__ float left(float p, float cut) {
+        if constexpr (BF16) return __builtin_fmaf(p, 1.f + 0x1p-23f, -cut);
+        else return __builtin_amdgcn_fmed3f(p - cut, 0x1p-24f, p);
     }
     // V^T of 16 channels and 32 keys, as the operand of the second product: elements 0..3 and 4..7 of lane l are keys 4 (l / 16) + 0..3 and
     // 16 more.
@@ -246,10 +253,9 @@ struct flash {
                     if constexpr (TERMS == 1) {
                         pf[n][0][j][e] = pack<BF16>(p[2 * e], p[2 * e + 1]);
                     } else {
-                        constexpr float MORE = 1.f + 0x1p-23f;
                         const uint32_t cut = cut_pair<BF16>(p[2 * e], p[2 * e + 1]);
                         pf[n][0][j][e] = (int)cut;
-                        pf[n][1][j][e] = pack<BF16>(__builtin_fmaf(p[2 * e], MORE, -value_of<BF16>(cut & 0xffffu)), __builtin_fmaf(p[2 * e + 1], MORE, -value_of<BF16>(cut >> 16)));
+                        pf[n][1][j][e] = pack<BF16>(left(p[2 * e], value_of<BF16>(cut & 0xffffu)), left(p[2 * e + 1], value_of<BF16>(cut >> 16)));
                     }
                 }
             }
@@ -342,7 +348,7 @@ __device__ __forceinline__ void join_waves(F& f, int n, float* os, float (*top)[
         for (int w = 0; w < W; ++w) {
             const float g = top[w][r] == -INFINITY ? 0.f * sum[w][r] : __builtin_amdgcn_exp2f(top[w][r] - big);   // a sum that is no number stays
             z += g * sum[w][r];
-            if (g > 0.f || g != g) y += g * *reinterpret_cast<const v4f*>(os + (w * 16 + r) * OLD + c);
+            y += g * *reinterpret_cast<const v4f*>(os + (w * 16 + r) * OLD + c);      // so does an infinite value, as none, where g is 0
         }
         put(r, c, y, big, z);
     }
@@ -709,7 +715,7 @@ __global__ __launch_bounds__(64 * W, DP > 128 ? 1 : 2) void attend_finish_kernel
         f.weigh(a.scale_log2, &sees, false);
         f.add(vs + c0);
         if (odd) {
-            // One drafted token at a time: its values that are not numbers alone in LDS, and only the rows that weigh it take the product.
+            // One drafted token at a time: its values that are not numbers alone in LDS, and only the rows that see it take the product.
 #pragma unroll 1
             for (int j = 0; j < 32; ++j) {
                 if (!(there >> j & 1u)) continue;
@@ -723,14 +729,10 @@ __global__ __launch_bounds__(64 * W, DP > 128 ? 1 : 2) void attend_finish_kernel
                     }
                 f.put_v(vs, 1u << j);
                 v4i alone = {0, 0, 0, 0};
-                uint32_t any = 0;
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    if (e / 4 * 16 + quad * 4 + e % 4 == j) {
-                        any = (uint32_t)f.pf[0][0][0][e / 2] & (e % 2 ? 0xffff0000u : 0xffffu);
-                        alone[e / 2] = (int)any;
-                    }
-                const bool takes = rows_max(any ? 1.f : 0.f) > 0.f;
+                    if (e / 4 * 16 + quad * 4 + e % 4 == j) alone[e / 2] = (int)((uint32_t)f.pf[0][0][0][e / 2] & (e % 2 ? 0xffff0000u : 0xffffu));
+                const bool takes = sees >> j & 1u;
 #pragma unroll
                 for (int c = 0; c < state::CT; ++c) {
                     const v4f x = mfma<BF16>(f.get_v(vs + c0, c), alone, v4f{0.f, 0.f, 0.f, 0.f});

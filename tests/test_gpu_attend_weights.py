@@ -1,5 +1,5 @@
-"""Attention over a paged cache where small weights decide, and where nothing is weighed: every stream's row holds the same pages, so that one part of
-the work is a whole long context."""
+"""Attention over a paged cache where small weights decide, and infinite values that are weighed: every stream's row holds the same pages, so that
+one part of the work is a whole long context."""
 import math
 
 import pytest
@@ -78,6 +78,78 @@ def test_one_key_far_above_many(sw, dtype, d, T, G, gap, spread):
         bad = (out[b, i, h].double() - want).abs() / tol
         assert (bad <= 1).all(), f"off by {bad.max():.3g} tolerances, {((out[b, i, h].double() - want).abs() / want.abs()).max():.3g} of the value"
         assert abs(float(lse[b, i, h]) - (s.max() + p.sum().log()).item()) <= e + (n / 4 + 64) * 2.0 ** -24 + 2.0 ** -22 * (1 + gap)
+
+
+def gaps(octaves, count, t):
+    """Keys' first channel for scores between two numbers of octaves below 0, whole octaves among them."""
+    g = torch.Generator().manual_seed(count)
+    x = torch.rand(count, generator=g) * (octaves[1] - octaves[0]) + octaves[0]
+    x[::4] = x[::4].round()
+    return (-x * math.log(2)).to(t)
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("T,G,d", [(1, 4, 64), (1, 32, 64), (10, 4, 64), (24, 8, 64), (1, 4, 256), (5, 4, 256)])
+def test_infinite_values_of_the_context_that_weigh_little(sw, dtype, T, G, d):
+    """An infinite value of a weight down to 2^-22 of the largest makes the result infinite: fp16 holds a weight from 2^-24 on, the largest being 2^11 at least."""
+    from paper_2603_17803_amd import binding
+    t, B, page = TYPES[dtype], 200, 16
+    k = torch.zeros((1, B, 1, page, d), dtype=t)
+    k[0, :, 0, 5, 0] = gaps((1, 22), B, t)
+    v = torch.ones((1, B, 1, page, d), dtype=t)
+    v[0, :, 0, 5, 2], v[0, :, 0, 5, 3] = math.inf, -math.inf
+    q = torch.zeros((B, T, G, d), dtype=t)
+    q[..., 0] = 1.0
+    table = torch.arange(B, dtype=torch.int32, device="cuda").view(B, 1)
+    out, _ = attend(sw, binding.Cache(k.cuda(), v.cuda(), table, torch.full((B,), page, dtype=torch.int32, device="cuda")), q)
+    assert (out[..., 2] == math.inf).all() and (out[..., 3] == -math.inf).all()
+    assert ((out[..., 4].double() - 1.0).abs() <= 2 * torch.finfo(t).eps).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("d", [64, 200])
+def test_infinite_values_of_drafted_tokens_that_weigh_little(sw, dtype, d):
+    """Infinite from any weight that the type holds, never finite where it is seen, and nothing to those who do not see it."""
+    t, B, T, G = TYPES[dtype], 200, 6, 3
+    n = 40
+    cache = shared_rows(torch.zeros((n, d), dtype=t), torch.ones((n, d), dtype=t), B)
+    k_new, v_new = torch.zeros((B, T, 1, d), dtype=t), torch.ones((B, T, 1, d), dtype=t)
+    q = torch.zeros((B, T, G, d), dtype=t)
+    q[..., 0] = 1.0
+    sees = torch.tensor([1 << i | (1 << 2 if i in (2, 4, 5) else 0) for i in range(T)], dtype=torch.int32).expand(B, T).contiguous().view(B, T, 1)
+    for octaves, held in (((1, 22), True), ((22, 60), False), ((200, 300), False)):
+        k_new[:, 2, 0, 0] = gaps(octaves, B, t)
+        v_new[:, 2, 0, 2] = math.inf
+        out, _ = attend(sw, cache, q, k_new=k_new.cuda(), v_new=v_new.cuda(), mask=sees.cuda())
+        seen = out[:, [2, 4, 5], :, 2]
+        assert (seen == math.inf).all() if held else ((seen == math.inf) | seen.isnan()).all()
+        finite = out.clone()
+        finite[:, [2, 4, 5], :, 2] = 1.0
+        assert ((finite.double() - 1.0).abs() <= 2 * torch.finfo(t).eps).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("T,G,d", [(1, 4, 64), (10, 8, 64), (3, 2, 256), (70, 1, 64), (70, 2, 136)])
+def test_infinite_values_among_weights_that_are_nothing(sw, dtype, T, G, d):
+    """Keys of which 32 in a row weigh 2^-250 of the others, one with an infinite value: never finite, in the context or among the drafted tokens."""
+    t, n = TYPES[dtype], 130
+    far = -250 * math.log(2)
+    k, v = torch.zeros((n, d), dtype=t), torch.ones((n, d), dtype=t)
+    k[32:64, 0], v[40, 2] = far, math.inf
+    q = torch.zeros((2, T, G, d), dtype=t)
+    q[..., 0] = 1.0
+    more = {}
+    if T > 64:
+        k_new, v_new = torch.zeros((2, T, 1, d), dtype=t), torch.ones((2, T, 1, d), dtype=t)
+        k_new[:, 32:64, 0, 0], v_new[:, 50, 0, 3] = far, -math.inf
+        more = dict(k_new=k_new.cuda(), v_new=v_new.cuda())
+    for B in (1, 2):
+        out, _ = attend(sw, shared_rows(k, v, B), q[:B].contiguous(), **{x: y[:B].contiguous() for x, y in more.items()})
+        assert not out[..., 2].isfinite().any()
+        if T > 64:
+            assert out[:, :50, :, 3].isfinite().all() and not out[:, 50:, :, 3].isfinite().any()
+        rest = out[..., [0, 1] + list(range(4, d))]
+        assert ((rest.double() - 1.0).abs() <= 2 * torch.finfo(t).eps).all()
 
 
 @pytest.mark.parametrize("dtype", ["fp16", "bf16"])
