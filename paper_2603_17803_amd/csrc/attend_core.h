@@ -94,6 +94,10 @@ __device__ __forceinline__ float rows_sum(float x) {
 // The same value in all lanes, said so: it stays in scalar registers and its branches are branches.
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
+// Between lanes of a wave that hand one another values through LDS: what was written before is written, and what was read is read.  The wave's LDS accesses
+// run in order, so it costs nothing; it holds the compiler to that order.
+__device__ __forceinline__ void wave_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
+
 // What a stream brings: the tokens it holds, slots of its selection (or tokens), drafted tokens, units of a (head, tile).
 struct stream {
     int len, slots, drafted, units;
@@ -491,12 +495,16 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attend_context_kernel(a
                     const uint32_t* ahead = mine + min(u + 1, n - 1) * UNIT;
                     auto next = [&](int key) { return ahead[key]; };
                     f.put_k(vs, a.d);
+                    wave_fence();
                     f.load(f.kr, kp, a.d, next);
                     f.template scores<state::KLD>(vs);
+                    wave_fence();
                     f.put_v(vs, there);
+                    wave_fence();
                     f.load(f.vr, vp, a.d, next);
                     f.weigh(a.scale_log2, &there, there == ~0u);
                     f.add(vs);
+                    wave_fence();
                 }
             }
             // along the line a step goes to the next pair or to the next part: their sum names what a part found for a pair
@@ -709,11 +717,15 @@ __global__ __launch_bounds__(64 * W, DP > 128 ? 1 : 2) void attend_finish_kernel
                 }
         }
         f.put_k(vs, a.d);
+        wave_fence();
         f.template scores<state::KLD>(vs);
+        wave_fence();
         f.put_v(vs, there);
+        wave_fence();
         const uint32_t sees = word & there;
         f.weigh(a.scale_log2, &sees, false);
         f.add(vs + c0);
+        wave_fence();
         if (odd) {
             // One drafted token at a time: its values that are not numbers alone in LDS, and only the rows that see it take the product.
 #pragma unroll 1
@@ -728,6 +740,7 @@ __global__ __launch_bounds__(64 * W, DP > 128 ? 1 : 2) void attend_finish_kernel
                         f.vr[i][e] = (int)(((y & EXP) == EXP ? y & 0xffffu : 0u) | ((y & EXP << 16) == EXP << 16 ? y & 0xffff0000u : 0u));
                     }
                 f.put_v(vs, 1u << j);
+                wave_fence();
                 v4i alone = {0, 0, 0, 0};
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
@@ -739,6 +752,7 @@ __global__ __launch_bounds__(64 * W, DP > 128 ? 1 : 2) void attend_finish_kernel
 #pragma unroll
                     for (int r = 0; r < 4; ++r) f.o[0][c][r] += takes ? x[r] : 0.f;
                 }
+                wave_fence();
             }
         }
         j0 += 32 * W;
