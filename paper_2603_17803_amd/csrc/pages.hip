@@ -165,10 +165,10 @@ __global__ __launch_bounds__(256) void fork_fill_kernel(fork_args a) {
     }
 }
 
-// The same in one workgroup, for tables of up to 4096 slots (16 waves' rows in pieces of 64, four a wave) and pools that LDS holds: what bounds a small
-// fork is launches and the trips to memory between them.  A wave has every 16th row, and holds its rows' slots in registers.  (4 rows of 64 slots:
+// The same in one workgroup, for tables of up to 4096 slots (16 waves' rows in pieces of 64, four a wave, so 64 rows at most) and pools that LDS holds: what bounds
+// a small fork is launches and the trips to memory between them.  A wave has every 16th row, and holds its rows' slots in registers.  (4 rows of 64 slots:
 // 7 us here, 20 by the four kernels; 256 rows of 128 slots, with more turns a wave: 100 here, 22 there.)
-constexpr int ONE_ROWS = 1024, ONE_SLOTS = 4, ONE_PAGES = 8192;
+constexpr int ONE_SLOTS = 4, ONE_ROWS = 16 * ONE_SLOTS, ONE_PAGES = 8192;
 __global__ __launch_bounds__(1024) void fork_one_kernel(fork_args a) {
     __shared__ int refs[ONE_PAGES], ids[ONE_PAGES];
     __shared__ int held[ONE_ROWS], kids[ONE_ROWS], eldest[ONE_ROWS], lens[ONE_ROWS], rooms[ONE_ROWS], parents[ONE_ROWS];
@@ -186,11 +186,13 @@ __global__ __launch_bounds__(1024) void fork_one_kernel(fork_args a) {
     const int mine = t < a.rows ? parent_of(a, t) : -1, room = t < a.rows && a.room ? max(a.room[t], 0) : 0, had = t < a.rows ? a.len[t] : 0;
     if (t < a.rows && a.parent[t] != mine) atomicOr(a.flags, SWARM_DEV_BAD_ENTRY);
     for (int i = t; i < a.P; i += 1024) refs[i] = a.refs[i];
-    held[t] = a.cap;
-    parents[t] = mine;
-    rooms[t] = room;
-    kids[t] = 0;
-    eldest[t] = a.rows;
+    if (t < a.rows) {
+        held[t] = a.cap;
+        parents[t] = mine;
+        rooms[t] = room;
+        kids[t] = 0;
+        eldest[t] = a.rows;
+    }
     __syncthreads();
     if (mine >= 0) atomicAdd(&kids[mine], 1), atomicMin(&eldest[mine], t);
     {
@@ -219,15 +221,15 @@ __global__ __launch_bounds__(1024) void fork_one_kernel(fork_args a) {
     const int len = mine >= 0 ? lens[mine] : 0, need = mine >= 0 ? need_of(len, room) : 0;
     const int kept = mine < 0 ? 0 : eldest[mine] == t ? min(held[mine], need) : len / a.page;
     if (mine >= 0 && (int64_t)len + room > (int64_t)a.cap * a.page) atomicOr(a.flags, SWARM_DEV_NO_PAGE);
-    new_kept[t] = kept;
-    new_need[t] = need;
     if (t < a.rows) {
+        new_kept[t] = kept;
+        new_need[t] = need;
         old_full[t] = lens[t] / a.page;
         old_kept[t] = kids[t] ? min(held[t], need_of(lens[t], rooms[eldest[t]])) : 0;
     }
     int want;
     const int before = block_excl_scan(t < a.rows ? need - kept : 0, waves, &want);
-    start[t] = before;
+    if (t < a.rows) start[t] = before;
     __syncthreads();
     {
         int r = wave, c = 0;
@@ -515,7 +517,7 @@ swarm_status swarm_cache_fork(swarm_ctx* ctx, const swarm_cache* c, const int32_
     a.flags = ctx->dev_flags;
     a.L = c->L, a.P = c->P, a.H = c->H, a.page = c->page, a.chunks = c->d / 8, a.rows = c->rows, a.cap = c->cap;
     const int turns = (c->rows + 15) / 16 * ((c->cap + 63) / 64);       // slots of a lane where one workgroup has all rows
-    if (c->rows <= ONE_ROWS && c->P <= ONE_PAGES && turns <= ONE_SLOTS) {
+    if (c->P <= ONE_PAGES && turns <= ONE_SLOTS) {
         hipLaunchKernelGGL(fork_one_kernel, dim3(1), dim3(1024), 0, ctx->stream, a);
     } else {
         hipLaunchKernelGGL(copy_words_kernel, dim3((unsigned)((c->P + 255) / 256 < 1024 ? (c->P + 255) / 256 : 1024)), dim3(256), 0, ctx->stream, c->refs, refs_out, c->P);
