@@ -81,7 +81,7 @@ __device__ __forceinline__ int above(const u64* keys, int n, u64 key) {
     return c;
 }
 
-// Cuts a list in LDS of n different keys down to its k best, in order, by a workgroup of 256; `best` has room for 256 and k more.
+// Cuts a list in LDS of n different keys down to its k best (at most 128), in order, by a workgroup of 256; `best` has room for 258.
 // Returns how many are left.
 __device__ int trim(u64* list, int n, int k, u64* best, int* count) {
     const int t = threadIdx.x;
@@ -383,7 +383,7 @@ __global__ __launch_bounds__(1024) void beam_join_kernel(beam_args a) {
         if (finished && i == list * a.k) staged[i] = candidate(0.f, a.eos);
         if (i - list * a.k < (finished ? 1 : length[list])) scored[i] = score_of_key(beams[list], staged[i], finished);
     }
-    const bool searched = n_staged && a.k >= 4 && lists <= 24;
+    const bool searched = n_staged && a.k >= 4 && lists <= 16;
     if (searched) {
         for (int i = t; i < n_staged; i += 1024) places[i] = i % a.k;
         if (t < a.k) parent[t] = -1, token[t] = -1, best[t] = -INFINITY;
@@ -391,8 +391,9 @@ __global__ __launch_bounds__(1024) void beam_join_kernel(beam_args a) {
     __syncthreads();
     if (searched) {
         // A candidate's place is how many stand above it: in each list the first few, found by halving.  The lists are divided over as many threads
-        // as there are for a candidate.  Its work grows with the square of the lists, that of the rounds below with k: 64 groups of 16 lists take 54 us
-        // by rounds and 52 so for k = 16, 89 and 83 for k = 64, 130 and 120 for k = 128 (the whole call); 8 groups of 124 lists, k = 8, 21 and 127.
+        // as there are for a candidate.  Its work grows with the square of the lists, that of the rounds below with k.  The whole call, 64 groups, 32000
+        // bf16 logits, k = 4, 16, 32, 64: 16 lists 30.0, 36.4, 45.2, 64.3 us by rounds and 29.6, 35.1, 42.9, 61.1 so; 18 lists 41.0, 50.1, 60.1, 82.0 and 40.8,
+        // 50.4, 66.1, 92.4; 24 lists 44.9, 54.0, 63.8, 86.9 and 45.3, 58.1, 74.8, 110.
         const int shares = max(1, 1024 / n_staged);
         for (int x = t; x < n_staged * shares; x += 1024) {
             const int share = x / n_staged, i = x - share * n_staged, list = i / a.k, beam = beams[list];

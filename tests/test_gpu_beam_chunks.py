@@ -181,3 +181,15 @@ def test_values_that_are_not_numbers(sw, size):
         scores[2] = math.inf
         scores[3, 1] = math.nan
         check(sw, logits, scores, k)
+
+
+@pytest.mark.parametrize("B,K,V", [(3, 16, 300), (3, 17, 300), (64, 16, 5000), (2, 2, 30000), (1, 1, 68000)])
+@pytest.mark.parametrize("k", [3, 4, 31, 128])
+def test_sixteen_lists_and_seventeen(sw, B, K, V, k):
+    """Either side of how many lists are merged at once."""
+    logits, scores = noise(K + k, B, K, V)
+    check(sw, logits, scores, k)
+    check(sw, torch.round(logits), torch.zeros_like(scores), k)
+    check(sw, logits[:, :1].expand(B, K, V).contiguous(), torch.zeros_like(scores), k)
+    logits[0, K - 1], scores[0, 0] = -math.inf, -math.inf
+    check(sw, logits, scores, k)
