@@ -632,10 +632,18 @@ __global__ __launch_bounds__(64 * W, DP > 128 ? (W == 4 ? 2 : 1) : W * (16 * NR 
 
 // Workgroup (pair, 16 rows): the parts of the context, the drafted tokens, the end.  W waves share the parts and the drafted tokens: one
 // where a pair has few parts, as many rows fill the device then, or eight (four for wide heads, for their registers) where it has many.  Latency bounds it:
-// three trips to memory, the drafted tokens' products, the join.  (24 x 4 pairs of 168 rows, 3 parts each: 21 us with four waves, 10 with one; 8 pairs of 4
-// rows, 32 parts each: 25 with one, 10 with four, 8 with eight.)  Where that are few workgroups, two share the channels, each with all scores: 8 pairs of 64
-// rows and 131000 tokens 123 us in all, so 117, 4 rows and 4096 tokens 17.6 and 16.6; with more they only do the scores twice (8 pairs of 256 rows 188 and 192,
-// 96 pairs of 512 rows 226 and 302).
+// three trips to memory, the drafted tokens' products, the join.  Where that are few workgroups, two share the channels, each with all scores; with more they only
+// do the scores twice.  Which form is measured, 8 heads of 128 x 4 query heads, the whole call by one wave / eight / eight in two shares, us:
+//   workgroups  parts of a pair  (streams x tokens, context)
+//   32          64               1 x 16, 8000     42.5 / 32.1 / 26.0
+//   128         8                4 x 16, 1000     18.0 / 17.8 / 16.8
+//   128         32               1 x 64, 8000     45.5 / 40.3 / 38.4
+//   256         8                8 x 16, 8000     59.4 / 58.9 / 62.9
+//   256         16               2 x 64, 8000     48.9 / 47.1 / 51.8
+//   512         8                4 x 64, 8000     64.5 / 69.1 / 76.6
+//   128         4                16 x 1, 8000     93.6 / 93.4 / 93.1
+//   512         4                16 x 16, 8000    119 / 123 / 129
+//   8           8                1 x 1, 1000      14.1 / 13.2 / 13.7
 template <bool BF16, int DP, int W, int CS, bool FULL>
 __global__ __launch_bounds__(64 * W, DP > 128 ? 1 : 2) void attend_finish_kernel(attend_args a) {
     typedef own_keys<BF16, DP, 1, 2, FULL, CS> state;
@@ -798,8 +806,9 @@ void launch_attend(const attend_args& a, hipStream_t stream) {
     }
     constexpr int MANY = DP > 128 ? 4 : 8;      // eight waves would leave wide heads too few registers
     const unsigned pairs = (unsigned)(a.B * a.H), rows = (unsigned)((a.T * a.G + 15) / 16);
-    if ((a.parts - 1) / 4 < a.B * a.H && a.T <= 64) hipLaunchKernelGGL((attend_finish_kernel<BF16, DP, 1, 1, FULL>), dim3(pairs, rows), dim3(64), 0, stream, a);
-    else if ((int64_t)pairs * rows >= 128) hipLaunchKernelGGL((attend_finish_kernel<BF16, DP, MANY, 1, FULL>), dim3(pairs, rows), dim3(64 * MANY), 0, stream, a);
+    const int64_t groups = (int64_t)pairs * rows, each = (a.parts + (int64_t)pairs - 1) / pairs;   // parts of a pair
+    if (a.T <= 64 && (each <= 4 || (each <= 8 && groups >= 512))) hipLaunchKernelGGL((attend_finish_kernel<BF16, DP, 1, 1, FULL>), dim3(pairs, rows), dim3(64), 0, stream, a);
+    else if (groups > 128) hipLaunchKernelGGL((attend_finish_kernel<BF16, DP, MANY, 1, FULL>), dim3(pairs, rows), dim3(64 * MANY), 0, stream, a);
     else hipLaunchKernelGGL((attend_finish_kernel<BF16, DP, MANY, 2, FULL>), dim3(pairs, rows, 2), dim3(64 * MANY), 0, stream, a);
 }
 
