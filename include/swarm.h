@@ -412,9 +412,8 @@ typedef struct {
  * Products and sums are fp32, the sum of weights that of the fp32 weights.  A weight enters its product with v as two terms of the cache's type
  * (15 bits and more, so that the result is rounded once, at the end) where T*G <= 32 (16 for d > 128), and for the drafted tokens always; a
  * weight of the context beyond that is rounded to the type (off by half a step, as the result is by its own rounding).  fp16 has no numbers for the smallest
- * weights: there one is off by up to 2^-35 of the largest in any case. What a token does not
- * see never reaches its result, infinities and NaN included; an infinite value that it sees makes the result infinite, or NaN where its weight is below what
- * the type holds.
+ * weights: there one is off by up to 2^-35 of the largest in any case.  What a token does not see never reaches its result, infinities and NaN included; an
+ * infinite value that it sees makes the result infinite, or NaN where its weight is below what the type holds (bf16 2^-133, fp16 2^-35 of the largest).
  *
  * layer        which of the cache's L layers.
  * q            device, [B][T][H*G][d] in the cache's type, 16-byte aligned.   B <= rows streams, T drafted tokens each (1..256; one
@@ -432,6 +431,9 @@ typedef struct {
  * A page id outside [0,P) drops its tokens (SWARM_DEV_BAD_PAGE); a selected position outside [-1, cap) or [-1, cap * page) is
  * dropped (SWARM_DEV_BAD_ENTRY); a length outside [0, cap * page], or n_new outside [0, T], is cut to it (SWARM_DEV_BAD_LEN).
  * The order of sums depends on the sizes alone: the same call gives the same bits.
+ * Scratch: 4 (d' + 2) (B H R + S) bytes, with d' = d rounded up to 64, 96, 128, 192 or 256, R = T*G rounded up to 16, 32, 64, 128, 192 or 256 rows (d > 128: 16, 32,
+ * 64, 96 or 128; more are cut into equal tiles of at most that many, each rounded up) and S = min(512 R, 65536), or R where that is more: 100 MB for
+ * B = 64, H = 8, R = 256, d = 128.
  * Errors: SWARM_EINVAL for NULL or misaligned required pointers, one of k_new and v_new without the other, sizes out of range, cap *
  * page above 2^30, a layer of k, or k_new, of 64 GiB or more, B * H contexts of up to 2^31 times 128 keys or more (by the table's width, or
  * n_sel), out or lse overlapping an input.
@@ -457,7 +459,7 @@ swarm_status swarm_tree_attend(swarm_ctx* ctx, const swarm_cache* cache, int32_t
  *          pool's new pages are written in place.  A page that two rows with different parents hold partly filled stays shared: such
  *          tables do not come out of these calls.
  * A length outside what the row's leading pages hold is cut to it (SWARM_DEV_BAD_LEN); page ids outside [0,P) end a row there
- * (SWARM_DEV_BAD_PAGE).   Errors: SWARM_EINVAL for NULL or misaligned pointers, rows > 16384, rows * cap > 2^28, P > 2^26,
+ * (SWARM_DEV_BAD_PAGE).   Scratch: 24 bytes a row, 4 a page.   Errors: SWARM_EINVAL for NULL or misaligned pointers, rows > 16384, rows * cap > 2^28, P > 2^26,
  * overlapping outputs.
  */
 swarm_status swarm_cache_fork(swarm_ctx* ctx, const swarm_cache* cache, const int32_t* parent, const int32_t* room,
@@ -483,7 +485,7 @@ swarm_status swarm_cache_append(swarm_ctx* ctx, const swarm_cache* cache, const 
  * Compacting: the n pages in use (refs > 0) come to stand at ids 0..n-1.  Those with an id of n or more move, in ascending order, to
  * the free ids below n, in ascending order, in all layers; tables and counts follow.
  * table_out int32 [rows][cap], refs_out int32 [P], live int32 [1] (n): written whole; none may overlap an input.  Table entries
- * outside [0,P) stay as they are.  Errors: as swarm_cache_fork.
+ * outside [0,P) stay as they are.  Scratch: 12 bytes a page.  Errors: as swarm_cache_fork, but up to 65535 rows.
  */
 swarm_status swarm_cache_compact(swarm_ctx* ctx, const swarm_cache* cache, int32_t* table_out, int32_t* refs_out, int32_t* live);
 
@@ -503,6 +505,7 @@ swarm_status swarm_cache_compact(swarm_ctx* ctx, const swarm_cache* cache, int32
  *            [B*k][hist_cap]:  hist_out[r][0..step) = hist[parent[r]][0..step), hist_out[r][step] = token[r]; the rest, and rows without a
  *            parent, are left as they were.  A step outside [0, hist_cap) is cut to [0, hist_cap], its token not written and SWARM_DEV_BAD_ENTRY raised.  All three
  *            NULL: no histories.
+ * Scratch: (B*K + 1024) * (20 + 8 k) bytes.
  * Errors: SWARM_EINVAL for NULL or misaligned pointers, B, K, V, k < 1, K > 64, k > 128, V > 2^24, B * K > 2^20, stride < V, eos outside [0,V)
  * with finished, outputs that overlap an input.
  */

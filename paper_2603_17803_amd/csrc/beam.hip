@@ -5,7 +5,7 @@
 // cut down to its k best whenever it has grown.  The first bound is the k-th largest of the first chunk's maxima of 64 groups of threads (of 256 threads for
 // k above 32).  A logit costs its exponential, one comparison and one addition.  What bounds it is memory for fp32 (512 rows of 128000, k = 1: 52 us
 // with the second kernel, 5.0 TB/s), and with 16-bit logits the candidates: without the few that each chunk adds after the first, and the waits of
-// the other waves for the one that adds them, k = 16 takes 42 us in place of 54; the exponentials cost nothing.
+// the other waves for the one that adds them, k = 16 takes 42 us in place of 54; the exponentials cost one.
 //
 // A second kernel, a workgroup for each group of beams, merges the sorted lists and moves the histories.
 #include <math.h>
